@@ -285,6 +285,42 @@ int loopspec_time_linear_tc(const void* const* Ws, int32_t n_w, const float* x, 
 int loopspec_op_linear_static(const void* W, int32_t weight_dtype, const float* x, float* y, int32_t M, int32_t N,
                               int32_t K, void* cuda_stream);
 
+/* ---- operators between the linear maps of a serving step --------------------------------------------------------------
+ * For programs that drive a decode loop of their own on the linear maps above (the paper's own loop is loopspec_decode; these have no
+ * counterpart in it): a paged cache is filled from the rows of a QKV projection, attended to by a batch whose sequences share a prefix, and
+ * a token is drawn from every row of logits.  Stream-ordered on cuda_stream (the legacy default stream included), no synchronisation, no allocation,
+ * nothing kept between calls: they can be captured into a CUDA graph and replayed, and calls on different streams may overlap as long
+ * as they share neither outputs nor scratch.  All pointers are device memory of the current device unless said otherwise; types: 0 = fp32, 1 = bf16,
+ * 2 = fp16.  Shapes outside what is stated return LOOPSPEC_EINVAL, scratch that is missing, too small or not 256-byte aligned LOOPSPEC_ECAPACITY; neither
+ * launches anything.  What only the device can see is bounds-checked there: nothing outside the cache and the tables is read or written, and
+ * a flag is left - bit 0 a table entry that is no page of the cache, or a position beyond the table; bit 1 row counts that do not ascend in
+ * [0, T], or a length beyond the table; bit 2 a bounded wait that ran out. */
+
+/* Keys and values of one layer behind one set of strides: element (page, head, slot, i) of either lies at
+ * page * page_stride + head * head_stride + slot * slot_stride + i.  Position p of a sequence lies in page table[p / page_size], slot
+ * p % page_size.  page_size: a power of two up to 65536; head_dim % 8 == 0 and at most 256; k and v 16-byte aligned, strides multiples of 8 (elements). */
+typedef struct {
+  void *k, *v;
+  int64_t page_stride, head_stride, slot_stride;
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  int32_t dtype; /* 1 or 2 */
+} loopspec_paged_kv;
+
+/* Appends the T rows of a QKV projection to the cache.  qkv: [T] rows of qkv_dtype, qkv_ld elements apart, each n_q_heads query heads, then
+ * n_kv_heads key heads, then the value heads.  Rows cu_rows[b] .. cu_rows[b + 1] - 1 (int32 [n_seqs + 1], ascending from 0) are the next tokens of
+ * sequence b, which has cached[b] positions already: row j gets position cached[b] + j of page_table[b] (int32, table_width entries, rows table_ld
+ * apart).  Rows from cu_rows[n_seqs] on are padding: neither q nor the cache is touched for them.
+ * Queries and keys are multiplied by gain / sqrt(mean of the head's squares + eps) where a gain (q_norm, k_norm: fp32 [head_dim], or NULL) is given, then
+ * rotated: pairs (i, i + rot_dim / 2) of the first rot_dim elements turn by index * inv_freq[i] (fp64 [rot_dim / 2], radians per position;
+ * rot_dim % 8 == 0, 0 = no rotation), index = position + pos_offset[b] (int32 [n_seqs], NULL = 0: the length of a shared prefix, say).  The angle is taken
+ * in 64 bits, the rest in fp32 and rounded once to the cache's type; q_out: [T] rows of n_q_heads heads of that type, q_ld elements apart
+ * (n_q_heads = 0: keys and values only).  qkv and q_out: 16-byte aligned, rows multiples of 8 elements.  Row 0 of every sequence may be any number of
+ * positions; two sequences must not own the same page at the positions being written.  flag: int32 that the call ors its bits into, or NULL. */
+int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv,
+                          const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* cached, const int32_t* cu_rows, int32_t n_seqs,
+                          const int32_t* pos_offset, const double* inv_freq, int32_t rot_dim, const float* q_norm, const float* k_norm, float eps,
+                          void* q_out, int64_t q_ld, int32_t* flag, void* cuda_stream);
+
 const char* loopspec_last_error(loopspec_ctx*);
 int loopspec_destroy(loopspec_ctx*);
 

@@ -14,7 +14,7 @@ EXPORTS = ["loopspec_workspace_bytes", "loopspec_init", "loopspec_prefill", "loo
            "loopspec_get_stats", "loopspec_get_commits", "loopspec_get_row_trace", "loopspec_debug_logits",
            "loopspec_launches_per_step", "loopspec_decode_paths", "loopspec_debug_drop_tile", "loopspec_time_kernel", "loopspec_linear_scratch_bytes", "loopspec_op_linear",
            "loopspec_op_linear_static", "loopspec_linear_tc_scratch_bytes", "loopspec_op_linear_tc", "loopspec_time_linear_tc",
-           "loopspec_last_error", "loopspec_destroy"]
+           "loopspec_op_append_kv", "loopspec_last_error", "loopspec_destroy"]
 
 STATUS = {0: "OK", -1: "EINVAL", -2: "ESTATE", -3: "ECAPACITY", -4: "ECUDA", -5: "ETIMEOUT", -6: "EUNSUPPORTED"}
 
@@ -55,6 +55,11 @@ class Stats(C.Structure):
                [("gamma", C.c_double), ("tv_d1", C.c_double), ("tv_d2", C.c_double), ("tv_n1", C.c_int64), ("tv_n2", C.c_int64)]
 
 
+class PagedKv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH) or _build.needs_build():
         try:
@@ -92,6 +97,8 @@ def _load():
     lib.loopspec_op_linear_tc.argtypes = [V, V, V, I, I, I, V, C.c_size_t, V]
     lib.loopspec_time_linear_tc.argtypes = [C.POINTER(V), I, V, I, I, I, V, C.c_size_t, I, C.POINTER(C.c_float), V]
     lib.loopspec_op_linear_static.argtypes = [V, I, V, V, I, I, I, V]
+    L = C.c_int64
+    lib.loopspec_op_append_kv.argtypes = [V, I, L, I, I, P(PagedKv), V, L, I, V, V, I, V, V, I, V, V, C.c_float, V, L, V, V]
     lib.loopspec_last_error.restype = C.c_char_p
     lib.loopspec_last_error.argtypes = [V]
     lib.loopspec_destroy.argtypes = [V]
