@@ -321,6 +321,23 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
                           const int32_t* pos_offset, const double* inv_freq, int32_t rot_dim, const float* q_norm, const float* k_norm, float eps,
                           void* q_out, int64_t q_ld, int32_t* flag, void* cuda_stream);
 
+/* Attention of T new rows of n_seqs sequences that share a prefix: row j (of n) of sequence b, one of cu_rows[b] .. cu_rows[b + 1] - 1, attends to the
+ * prefix - prefix_len positions in the pages prefix_pages (int32 [ceil(prefix_len / page_size)]) - and to the sequence's own positions
+ * below lens[b] - (n - 1 - j) of page_table[b] (own position 0 in its first page; lens[b] counts the new rows, appended beforehand, so the
+ * last row sees all of them).  out = softmax(scale * q K^T) V per query head, heads n_q_heads / n_kv_heads to a key head; scale 0 = 1 / sqrt(head_dim).
+ * The prefix's keys and values are read and multiplied once for all sequences.  A row that sees no key gets zeros (lse -inf).  Keys and values behind
+ * what a row sees do not enter it, whatever they hold.  q, out: [T] rows of n_q_heads heads of the cache's type, q_ld / out_ld
+ * elements apart, 16-byte aligned, multiples of 8 elements; lse: fp32 [T][n_q_heads], the natural logarithm of the sum of the exponentials, or NULL.  Rows from cu_rows[n_seqs]
+ * on are left as they are.  head_dim 64 or 128; n_seqs <= 2048; prefix_len >= 0.  Scores, sums and weighted values are fp32; the
+ * softmax weights are rounded to the cache's type before they multiply the values.  scratch: loopspec_prefix_attention_scratch_bytes bytes (0 = not a shape it
+ * takes), contents irrelevant; calls in flight at the same time need scratch of their own.  Deterministic; how the sums are cut depends on the batch.  flag:
+ * int32 that the call ors its bits into, or NULL; outputs of a call that left a bit there are void where the fault lay. */
+size_t loopspec_prefix_attention_scratch_bytes(int32_t T, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t prefix_len);
+int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv, const int32_t* prefix_pages,
+                                 int32_t prefix_len, const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* lens,
+                                 const int32_t* cu_rows, int32_t n_seqs, float scale, void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch,
+                                 size_t scratch_bytes, void* cuda_stream);
+
 const char* loopspec_last_error(loopspec_ctx*);
 int loopspec_destroy(loopspec_ctx*);
 

@@ -3,9 +3,12 @@
 #include "../../include/loopspec.h"
 
 #include <algorithm>
+#include <atomic>
+#include <cmath>
 #include <cstring>
 
 #include "op_append.cuh"
+#include "op_attention.cuh"
 
 using namespace ls;
 
@@ -66,6 +69,59 @@ AppendFn append_fn(int dtype, int lh) {
   return dtype == 0 ? append_fn<float, TO>(lh) : dtype == 1 ? append_fn<__nv_bfloat16, TO>(lh) : append_fn<__half, TO>(lh);
 }
 
+constexpr int kSms = 148;
+
+// Lets a kernel ask for `bytes` of dynamic shared memory; `done` remembers, a bit per device, that it may
+bool allow_smem(const void* fn, int bytes, std::atomic<unsigned long long>& done) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  if (dev < 64) done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
+}
+
+// ---- attention behind a shared prefix ----
+struct PxPlan {
+  int n_warps, max_tiles, prefix_rows;
+  size_t plan_off, item_ml, item_o, warp_ml, warp_o, total;
+};
+bool px_plan(int T, int B, int nq, int nkv, int d, int P, PxPlan* o) {
+  if (T < 0 || B < 0 || B > PXR_MAX_SEQS || nq < 1 || nkv < 1 || nq % nkv || (d != 64 && d != 128) || P < 0) return false;
+  if ((int64_t)T * nq > (1 << 27) || nkv > 65535) return false;
+  const int G = nq / nkv, rows = T * G;
+  o->prefix_rows = P > 0;
+  o->n_warps = kSms * 2 * PXR_WARPS;
+  o->max_tiles = rows / 16 + B + (o->prefix_rows ? rows / 16 + 1 : 0);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t r = at;
+    at += (n + 255) / 256 * 256;
+    return r;
+  };
+  o->plan_off = take((size_t)(2 * (B + 1) + 2) * 4);
+  o->item_ml = take((size_t)nkv * o->max_tiles * 128);
+  o->item_o = take((size_t)nkv * o->max_tiles * 16 * d * 4);
+  o->warp_ml = take((size_t)o->n_warps * 128);
+  o->warp_o = take((size_t)o->n_warps * 16 * d * 4);
+  o->total = at;
+  return true;
+}
+template <typename T, int D>
+int px_launch(PrefixParams& p, void* stream) {
+  static std::atomic<unsigned long long> allowed;
+  const int NP = p.B + p.prefix_rows;
+  if (!allow_smem((const void*)prefix_rows_kernel<T, D>, px_rows_smem(D, PXR_MAX_SEQS + 1), allowed)) return LOOPSPEC_ECUDA;
+  const int rc = launch(prefix_rows_kernel<T, D>, dim3(kSms * 2), PXR_WARPS * 32, px_rows_smem(D, NP), stream, p);
+  if (rc) return rc;
+  const int z = std::max(1, std::min(16, (int)(((int64_t)p.T * p.G / p.B + 3) / 4)));
+  return launch(prefix_merge_kernel<T, D>, dim3(p.kv.n_kv, p.B, z), 128, 0, stream, p, true);
+}
+
 }  // namespace
 
 extern "C" {
@@ -94,6 +150,43 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
   const int per_cta = APP_WARPS * (32 / lh), iters = (int)((n_q_heads + 2 * (int64_t)p.kv.n_kv + per_cta - 1) / per_cta);
   const int split = std::max(1, std::min(iters, 1184 / T));
   return launch(fn, dim3(T, split), APP_WARPS * 32, 0, cuda_stream, p);
+}
+
+size_t loopspec_prefix_attention_scratch_bytes(int32_t T, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t prefix_len) {
+  PxPlan t;
+  return px_plan(T, n_seqs, n_q_heads, n_kv_heads, head_dim, prefix_len, &t) ? t.total : 0;
+}
+
+int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv, const int32_t* prefix_pages,
+                                 int32_t prefix_len, const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* lens,
+                                 const int32_t* cu_rows, int32_t n_seqs, float scale, void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch,
+                                 size_t scratch_bytes, void* cuda_stream) {
+  PrefixParams p;
+  memset(&p, 0, sizeof p);
+  PxPlan t;
+  if (!paged_kv(kv, &p.kv) || !px_plan(T, n_seqs, n_q_heads, p.kv.n_kv, p.kv.d, prefix_len, &t) || !(scale >= 0.f) || std::isinf(scale)) return LOOPSPEC_EINVAL;
+  if (table_width < 0 || table_ld < table_width || (int64_t)table_width * kv->page_size > INT32_MAX) return LOOPSPEC_EINVAL;
+  if (T == 0 || n_seqs == 0) return LOOPSPEC_OK;  // (every row is padding)
+  const int64_t width = (int64_t)n_q_heads * p.kv.d;
+  if (!q || !aligned16(q) || q_ld % 8 || (T > 1 && q_ld < width) || !out || !aligned16(out) || out_ld % 8 || (T > 1 && out_ld < width)) return LOOPSPEC_EINVAL;
+  if (!lens || !cu_rows || (table_width && !page_table) || (prefix_len && !prefix_pages)) return LOOPSPEC_EINVAL;
+  p.G = n_q_heads / p.kv.n_kv;
+  // units of 16 keys x 16 rows of a kv head, counted in 32 bits
+  const double units = ((double)T * p.G / 16 + n_seqs) * ((double)table_width * kv->page_size / 16 + 1) + ((double)T * p.G / 16 + 1) * ((double)prefix_len / 16 + 1);
+  if (units >= 2147483648.0) return LOOPSPEC_EINVAL;
+  if (!scratch || scratch_bytes < t.total || (reinterpret_cast<uintptr_t>(scratch) & 255)) return LOOPSPEC_ECAPACITY;
+  p.q = q, p.q_ld = q_ld, p.prefix_pages = prefix_pages, p.prefix_len = prefix_len, p.prefix_rows = t.prefix_rows;
+  p.page_table = page_table, p.table_ld = table_ld, p.table_w = table_width, p.lens = lens, p.cu_rows = cu_rows;
+  p.B = n_seqs, p.T = T, p.nq = n_q_heads;
+  p.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)p.kv.d) : scale) * 1.4426950408889634f;
+  p.max_tiles = t.max_tiles, p.n_warps = t.n_warps;
+  unsigned char* sc = static_cast<unsigned char*>(scratch);
+  p.plan = reinterpret_cast<int*>(sc + t.plan_off);
+  p.item_ml = reinterpret_cast<float*>(sc + t.item_ml), p.item_o = reinterpret_cast<float*>(sc + t.item_o);
+  p.warp_ml = reinterpret_cast<float*>(sc + t.warp_ml), p.warp_o = reinterpret_cast<float*>(sc + t.warp_o);
+  p.out = out, p.out_ld = out_ld, p.lse = lse, p.flag = flag;
+  if (p.kv.d == 128) return kv->dtype == 1 ? px_launch<__nv_bfloat16, 128>(p, cuda_stream) : px_launch<__half, 128>(p, cuda_stream);
+  return kv->dtype == 1 ? px_launch<__nv_bfloat16, 64>(p, cuda_stream) : px_launch<__half, 64>(p, cuda_stream);
 }
 
 }  // extern "C"

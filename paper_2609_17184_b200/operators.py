@@ -99,3 +99,57 @@ def append_kv(qkv, k_cache, v_cache, page_table, cached, cu_rows, n_q_heads, inv
           _vec(inv_freq, "inv_freq", torch.float64, rot // 2, dev), rot, _vec(q_norm, "q_norm", torch.float32, d, dev),
           _vec(k_norm, "k_norm", torch.float32, d, dev), eps, out.data_ptr(), out.stride(0), _vec(flag, "flag", torch.int32, 1, dev))
     return out
+
+
+def prefix_attention_scratch_bytes(T, n_seqs, n_q_heads, n_kv_heads, head_dim, prefix_len):
+    return lib.loopspec_prefix_attention_scratch_bytes(T, n_seqs, n_q_heads, n_kv_heads, head_dim, prefix_len)
+
+
+def prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, lens, cu_rows, scale=None, out=None, lse=None, scratch=None, flag=None):
+    """Attention of a batch whose sequences share a prefix; returns (out [T, n_q, d], lse fp32 [T, n_q]).
+
+    q [T, n_q, d] in the cache's type; k_cache, v_cache [pages, n_kv, page_size, d] bf16 / fp16 (views of any strides), d 64 or 128; prefix_pages
+    int32 [>= ceil(prefix_len / page_size)] (None without a prefix); page_table [B, W], lens [B], cu_rows [B + 1] int32: the sequences' own pages, how
+    many own positions they hold (the new rows included) and where their rows begin.  Row j of n sees the prefix and the own positions below lens - (n
+    - 1 - j).  scale: None = 1 / sqrt(d).  Rows behind cu_rows[B] are left as they are.  scratch: uint8, 256-byte aligned,
+    prefix_attention_scratch_bytes (allocated here if None).  flag: int32 tensor of one element that bits are or-ed into when a page lies outside the cache
+    (1), lengths or row counts are not what they should be (2) or a bounded wait ran out (4)."""
+    dev = q.device
+    if dev.type != "cuda":
+        _bad("q: a CUDA tensor is needed")
+    kv = _paged(k_cache, v_cache, dev)
+    _need(q, "q", k_cache.dtype, 3, dev)
+    table = _table(page_table, dev)
+    T, nq, d = q.shape
+    B = page_table.size(0)
+    if d != kv.head_dim or (q.stride(1) != d and nq > 1 and T):
+        _bad("q: [T, n_q_heads, head_dim] with contiguous heads is needed")
+    if out is None:
+        out = torch.empty((T, nq, d), dtype=q.dtype, device=dev)
+    else:
+        _need(out, "out", q.dtype, 3, dev)
+        if out.shape != q.shape or (out.stride(1) != d and nq > 1 and T):
+            _bad("out: [T, n_q_heads, head_dim] with contiguous heads is needed")
+    if lse is None:
+        lse = torch.empty((T, nq), dtype=torch.float32, device=dev)
+    else:
+        _need(lse, "lse", torch.float32, 2, dev)
+        if lse.shape != (T, nq) or not lse.is_contiguous():
+            _bad("lse: [T, n_q_heads], contiguous, is needed")
+    pages = None
+    if prefix_len > 0:
+        _need(prefix_pages, "prefix_pages", torch.int32, 1, dev)
+        if prefix_pages.size(0) * kv.page_size < prefix_len:
+            _bad("prefix_pages: ceil(prefix_len / page_size) entries are needed")
+        pages = prefix_pages.data_ptr()
+    need = prefix_attention_scratch_bytes(T, B, nq, kv.n_kv_heads, d, prefix_len)
+    if need == 0:
+        _bad("prefix_attention: head_dim 64 or 128, n_q_heads a multiple of the key heads, at most 2048 sequences")
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+    else:
+        _need(scratch, "scratch", torch.uint8, 1, dev)
+    _call(lib.loopspec_op_prefix_attention, dev, "prefix_attention", q.data_ptr(), q.stride(0), T, nq, C.byref(kv), pages, prefix_len, *table,
+          _vec(lens, "lens", torch.int32, B, dev), _vec(cu_rows, "cu_rows", torch.int32, B + 1, dev), B, 0.0 if scale is None else scale, out.data_ptr(),
+          out.stride(0), lse.data_ptr(), _vec(flag, "flag", torch.int32, 1, dev), scratch.data_ptr(), scratch.numel(),)
+    return out, lse
