@@ -338,6 +338,17 @@ int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t
                                  const int32_t* cu_rows, int32_t n_seqs, float scale, void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch,
                                  size_t scratch_bytes, void* cuda_stream);
 
+/* One token for each of `rows` rows of logits (dtype 0, 1 or 2; ld elements apart), 1 <= vocab <= 262144, from one given uniform number a row (fp32 in [0, 1)).
+ * A token's weight is exp((z - max z) / temperature); tokens are ranked by logit, ties by lower index first.  top_k > 0 keeps the first top_k; 0 < top_p < 1 then the
+ * shortest prefix of the ranking whose share of what top-k kept reaches top_p; min_p > 0 then the tokens of at least min_p (at most 1) times the largest
+ * weight.  The token is the first, by index, at which the running sum of the kept weights exceeds uniform times their sum; its probability is its weight over that
+ * sum.  temperature <= 0 (or no number): the first of the largest logits, probability 1.  temperature, top_k, top_p, min_p: one value a row, or NULL for
+ * 1 / 0 / 1 / 0 throughout; other values than the stated switch a filter off.  A logit of -inf, or no number, is masked out; several of +inf share
+ * the weight; a row with nothing left gets token -1, probability 0.  Weights are taken in 64 bits and summed exactly, in multiples of 2^-S of the largest with S = min(48, 61 -
+ * ceil(log2 vocab)): the token is the one of the definition, whatever the order.  logits: any alignment of its type.  probs: NULL if not wanted. */
+int loopspec_op_sample(const void* logits, int32_t dtype, int64_t ld, int32_t rows, int32_t vocab, const float* uniforms, const float* temperature,
+                       const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* probs, void* cuda_stream);
+
 const char* loopspec_last_error(loopspec_ctx*);
 int loopspec_destroy(loopspec_ctx*);
 

@@ -7,4 +7,4 @@ device memory and streams.  There is no CPU fallback: importing fails if the lib
 from .binding import (LoopSpec, LoopSpecError, fit_envelope, lib, linear, linear_scratch_bytes, linear_static, linear_tc, time_linear_tc, max_branches,  # noqa: F401
                       pick_depths,
                       upload_weights, EXPORTS)
-from .operators import append_kv, prefix_attention, prefix_attention_scratch_bytes  # noqa: F401
+from .operators import append_kv, prefix_attention, prefix_attention_scratch_bytes, sample  # noqa: F401

@@ -9,6 +9,7 @@
 
 #include "op_append.cuh"
 #include "op_attention.cuh"
+#include "op_sample.cuh"
 
 using namespace ls;
 
@@ -24,14 +25,14 @@ int log2_of(int x) {
 
 // pdl: the kernel may start while its predecessor still runs and orders itself with griddepcontrol.wait
 template <typename P>
-int launch(void (*fn)(const P), dim3 grid, int block, size_t smem, void* stream, const P& params, bool pdl = false, int cluster = 1) {
+int launch(void (*fn)(const P), dim3 grid, int block, size_t smem, void* stream, const P& params, bool pdl = false, int cluster = 0) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = grid, cfg.blockDim = dim3(block), cfg.dynamicSmemBytes = smem, cfg.stream = static_cast<cudaStream_t>(stream);
   cudaLaunchAttribute at[2];
   int n = 0;
   if (pdl) at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization, at[n++].val.programmaticStreamSerializationAllowed = 1;
-  if (cluster > 1) {
+  if (cluster > 0) {
     at[n].id = cudaLaunchAttributeClusterDimension;
     at[n].val.clusterDim.x = cluster, at[n].val.clusterDim.y = 1, at[n].val.clusterDim.z = 1;
     ++n;
@@ -122,6 +123,18 @@ int px_launch(PrefixParams& p, void* stream) {
   return launch(prefix_merge_kernel<T, D>, dim3(p.kv.n_kv, p.B, z), 128, 0, stream, p, true);
 }
 
+// ---- sampling ----
+constexpr int SMP_MAX_VOCAB = 1 << 18, SMP_SMEM = 200 * 1024;
+template <typename T>
+int smp_launch(smp::Params& p, void* stream) {
+  static std::atomic<unsigned long long> allowed;
+  int cs = p.V >= 16384 ? 8 : p.V >= 4096 ? 4 : 1;
+  p.per = ((p.V + cs - 1) / cs + 7) / 8 * 8;
+  const int bytes = p.per * (int)sizeof(T) + 16;
+  if (!allow_smem((const void*)smp::sample_kernel<T>, SMP_SMEM, allowed)) return LOOPSPEC_ECUDA;
+  return launch(smp::sample_kernel<T>, dim3(p.rows * cs), smp::THREADS, bytes, stream, p, false, cs);
+}
+
 }  // namespace
 
 extern "C" {
@@ -187,6 +200,18 @@ int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t
   p.out = out, p.out_ld = out_ld, p.lse = lse, p.flag = flag;
   if (p.kv.d == 128) return kv->dtype == 1 ? px_launch<__nv_bfloat16, 128>(p, cuda_stream) : px_launch<__half, 128>(p, cuda_stream);
   return kv->dtype == 1 ? px_launch<__nv_bfloat16, 64>(p, cuda_stream) : px_launch<__half, 64>(p, cuda_stream);
+}
+
+int loopspec_op_sample(const void* logits, int32_t dtype, int64_t ld, int32_t rows, int32_t vocab, const float* uniforms, const float* temperature,
+                       const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* probs, void* cuda_stream) {
+  if (dtype < 0 || dtype > 2 || rows < 0 || rows > (1 << 24) || vocab < 1 || vocab > SMP_MAX_VOCAB || (rows > 1 && ld < vocab)) return LOOPSPEC_EINVAL;
+  if (rows == 0) return LOOPSPEC_OK;
+  if (!logits || !uniforms || !tokens || (reinterpret_cast<uintptr_t>(logits) & (dtype ? 1 : 3))) return LOOPSPEC_EINVAL;
+  smp::Params p;
+  memset(&p, 0, sizeof p);
+  p.logits = logits, p.ld = ld, p.rows = rows, p.V = vocab, p.shift = std::min(48, 61 - log2_of(vocab));
+  p.u = uniforms, p.temperature = temperature, p.top_k = top_k, p.top_p = top_p, p.min_p = min_p, p.token = tokens, p.prob = probs;
+  return dtype == 0 ? smp_launch<float>(p, cuda_stream) : dtype == 1 ? smp_launch<__nv_bfloat16>(p, cuda_stream) : smp_launch<__half>(p, cuda_stream);
 }
 
 }  // extern "C"

@@ -151,5 +151,28 @@ def prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, 
         _need(scratch, "scratch", torch.uint8, 1, dev)
     _call(lib.loopspec_op_prefix_attention, dev, "prefix_attention", q.data_ptr(), q.stride(0), T, nq, C.byref(kv), pages, prefix_len, *table,
           _vec(lens, "lens", torch.int32, B, dev), _vec(cu_rows, "cu_rows", torch.int32, B + 1, dev), B, 0.0 if scale is None else scale, out.data_ptr(),
-          out.stride(0), lse.data_ptr(), _vec(flag, "flag", torch.int32, 1, dev), scratch.data_ptr(), scratch.numel(),)
+          out.stride(0), lse.data_ptr(), _vec(flag, "flag", torch.int32, 1, dev), scratch.data_ptr(), scratch.numel())
     return out, lse
+
+
+def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None):
+    """One token per row of logits [rows, V] (fp32 / bf16 / fp16, V <= 262144) from given uniform numbers fp32 [rows]; returns (tokens int32 [rows],
+    their probabilities fp32 [rows]).
+
+    temperature, top_p, min_p fp32 [rows] and top_k int32 [rows], or None (1, off, off, off): the filters apply in the order top-k, top-p
+    (of what top-k kept), min-p; a temperature of 0 is the first of the largest logits.  -inf and NaN are masked out; a row of nothing else gets
+    token -1."""
+    dev = logits.device
+    if logits.dtype not in _DTYPE or dev.type != "cuda":
+        _bad("logits: a CUDA tensor of fp32, bf16 or fp16 is needed")
+    _need(logits, "logits", logits.dtype, 2, dev)
+    rows, V = logits.shape
+    if out is None:
+        out = torch.empty(rows, dtype=torch.int32, device=dev)
+    if probs is None:
+        probs = torch.empty(rows, dtype=torch.float32, device=dev)
+    _call(lib.loopspec_op_sample, dev, "sample", logits.data_ptr(), _DTYPE[logits.dtype], logits.stride(0), rows, V,
+          _vec(uniforms, "uniforms", torch.float32, rows, dev), _vec(temperature, "temperature", torch.float32, rows, dev),
+          _vec(top_k, "top_k", torch.int32, rows, dev), _vec(top_p, "top_p", torch.float32, rows, dev), _vec(min_p, "min_p", torch.float32, rows, dev),
+          _vec(out, "out", torch.int32, rows, dev), _vec(probs, "probs", torch.float32, rows, dev))
+    return out, probs
