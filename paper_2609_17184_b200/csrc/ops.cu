@@ -130,7 +130,8 @@ int smp_launch(smp::Params& p, void* stream) {
   static std::atomic<unsigned long long> allowed;
   int cs = p.V >= 16384 ? 8 : p.V >= 4096 ? 4 : 1;
   p.per = ((p.V + cs - 1) / cs + 7) / 8 * 8;
-  const int bytes = p.per * (int)sizeof(T) + 16;
+  p.hist_off = (p.per * (int)sizeof(T) + 16 + 15) / 16 * 16;
+  const int bytes = p.hist_off + smp::BINS * 4 + smp::LIST * 8;
   if (!allow_smem((const void*)smp::sample_kernel<T>, SMP_SMEM, allowed)) return LOOPSPEC_ECUDA;
   return launch(smp::sample_kernel<T>, dim3(p.rows * cs), smp::THREADS, bytes, stream, p, false, cs);
 }

@@ -87,6 +87,22 @@ def test_the_token_of_the_definition(mode, rows, V, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V,dt", [(50001, "bf16"), (128256, "fp32"), (20000, "fp32")])
+@pytest.mark.parametrize("spread", [0.0, 1e-3, 0.5, 6.0])
+def test_cuts_that_leave_thousands_of_tokens(V, dt, spread):
+    """Flat logits: top-k of thousands, a top-p that half of the vocabulary is needed for, and both."""
+    rng = np.random.default_rng(V)
+    rows = 12
+    z = torch.from_numpy(rng.standard_normal((rows, V)) * spread).to("cuda", DT[dt])
+    u = np.float32(rng.random(rows) * 0.99999)
+    k = rng.choice([2049, 5000, V // 2, V - 1], rows)
+    p = np.float32(rng.choice([0.3, 0.9, 0.9999], rows))
+    m = np.float32(rng.choice([0.0, 0.01, 0.9], rows))
+    for kw in ((None, k, None, None), (None, None, p, None), (None, k, p, m), (np.float32([0.01] * rows), k, p, None), (np.float32([50.0] * rows), k, p, None)):
+        check(z, u, call(z, u, *kw), *kw)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("V", [100, 20011])
 def test_ties_go_to_the_lower_index(V):
     """Few distinct values: the cut of top-k and top-p lies among equal logits, which the lower indexes survive."""
