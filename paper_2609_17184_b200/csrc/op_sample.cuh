@@ -2,11 +2,16 @@
 // lower index first); the token is the first, by index, at which the running sum of the kept weights exceeds u times their sum.
 //
 // Which side of a border a sum lies on decides the token, so no sum may depend on the order of its additions or lose what a 64-bit
-// evaluation keeps: a weight is evaluated in fp64 (2^y by a table of 2^(j/64) and a polynomial of degree 4: 4e-14) and rounded ONCE to a multiple
-// of 2^-S, S = 61 - ceil(log2 V) (44 at 128K tokens); from there on everything - sums over the vocabulary, p times a sum, u times a sum -
+// evaluation keeps: a weight is evaluated in fp64 (2^y by a table of 2^(j/256) and a polynomial of degree 3: 1.4e-13) and rounded ONCE to a multiple
+// of 2^-S, S = 61 - ceil(log2 V) (44 at 128K tokens, 48 at most); from there on everything - sums over the vocabulary, p times a sum, u times a sum -
 // is exact integer arithmetic.  Sums are the same in every order and for every number of CTAs.  A token below 2^-(S+1) of the best weighs nothing.
 //
-// A cluster of CTAs holds a row in shared memory: the logits are read from HBM once.
+// A cluster of CTAs holds a row in shared memory, so the logits are read from HBM once; what bounds a call is then the chain of passes over
+// a CTA's slice and of hand-overs in the cluster (some 1000 cycles each):
+//   1  load, largest logit                                                     all rows
+//   2  histogram over the distance from the best: tokens and places in a bin   rows with top-k or top-p
+//   3  exact mass, tokens of the bins where top-p may cut                      rows with top-p
+//   4  exact mass of what stays, by index                                      all rows of many kept tokens
 #pragma once
 #include <cooperative_groups.h>
 
@@ -19,9 +24,11 @@ typedef unsigned long long u64;
 
 constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int MAX_CS = 8;
-constexpr int NV = 7;  // sums taken together
+constexpr int NV = 7;              // sums taken together
 constexpr int BINS = 2 * THREADS;  // of the distance from the best logit, as far down as a token weighs anything
-constexpr int LIST = 2048;         // candidates that one CTA finishes alone
+constexpr int LIST = 2048;         // tokens one CTA can be sent, an equal part of them by each CTA
+constexpr int SOLO = 256;          // candidates with which one CTA finishes a row alone
+constexpr int MAX_VOCAB_BITS = 18;
 
 struct Params {
   const void* logits;
@@ -40,6 +47,11 @@ __device__ __forceinline__ unsigned key_of(float z) {
   const unsigned b = __float_as_uint(z + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float logit_of(unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+// a token's place in the ranking, ascending
+__device__ __forceinline__ u64 place_of(float z, int v) { return (u64)~key_of(z) << MAX_VOCAB_BITS | (unsigned)v; }
+__device__ __forceinline__ float logit_at(u64 place) { return logit_of(~(unsigned)(place >> MAX_VOCAB_BITS)); }
+__device__ __forceinline__ int token_at(u64 place) { return (int)((unsigned)place & ((1u << MAX_VOCAB_BITS) - 1)); }
 // fp32 -> fp64 by its bits (conversions run at a quarter of the rate of fp64 sums); zero comes out as 2^-127, infinity as 2^128: both are
 // what the sums here need
 __device__ __forceinline__ double widen(float z) {
@@ -63,26 +75,30 @@ __device__ __forceinline__ u64 times(float x, u64 m) {
 
 // the weight of a logit, scaled by 2^S
 struct Weigher {
-  const double* table;  // 2^(j / 64)
-  double top, c;        // largest logit, log2(e) / T
+  const double* table;  // 2^(j / 256)
+  double top, c;        // largest logit, 256 log2(e) / T
   int shift;
   float none;           // logits up to this one weigh nothing: -inf, or all finite ones beside an infinity
+  unsigned far;         // high word of -256 (S + 2): what lies further down is taken to lie there (and weighs nothing)
+  // No branch, so that the chains of neighbouring tokens overlap (one alone takes some 250 cycles).
   __device__ __forceinline__ double scaled(float z) const {
-    const double y = (widen(z) - top) * c;
-    if (!(z > none) || !(y > -(double)(shift + 2))) return 0.0;
-    const double magic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low word is 64 y to the nearest integer
-    const double t = fma(y, 64.0, magic);
+    double y = (widen(z) - top) * c;
+    // (y <= 0: a larger high word is further down; the low word does not matter there)
+    y = __hiloint2double((int)min(z > none ? (unsigned)__double2hiint(y) : 0xffffffffu, far), __double2loint(y));
+    const double magic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low word is y to the nearest integer
+    const double t = y + magic;
     const int k = __double2loint(t);
-    const double f = fma(t - magic, -1.0 / 64, y) * 0.69314718055994530942;  // 2^y = 2^(k / 64) e^f, |f| <= ln 2 / 128
-    const double q = fma(f, fma(f, fma(f, fma(f, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0);
-    const double w = table[k & 63];
-    return q * __hiloint2double(__double2hiint(w) + ((k >> 6) + shift) * (1 << 20), __double2loint(w));
+    const double f = y - (t - magic);  // 2^(y / 256) = 2^(k / 256) 2^(f / 256), |f| <= 1 / 2
+    constexpr double a = 0.69314718055994530942 / 256;
+    const double q = fma(f, fma(f, fma(f, a * a * a / 6, a * a / 2), a), 1.0);
+    const double w = table[k & 255];
+    return q * __hiloint2double(__double2hiint(w) + ((k >> 8) + shift) * (1 << 20), __double2loint(w));
   }
-  __device__ __forceinline__ u64 rounded(double w) const { return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull; }  // (below 2^52)
+  __device__ __forceinline__ static u64 rounded(double w) { return (u64)__double_as_longlong(w + 4503599627370496.0) & 0xfffffffffffffull; }  // (below 2^52)
   __device__ __forceinline__ u64 operator()(float z) const { return rounded(scaled(z)); }
 };
 
-// Sums, minima and maxima over the cluster: warps, then the CTA's partials in every CTA's memory, two sets of slots in turn
+// Sums and maxima over a CTA or the cluster: warps, then the CTA's partials in every CTA's memory, two sets of slots in turn
 struct Cluster {
   cg::cluster_group cl;
   int n, rank, phase;
@@ -90,7 +106,7 @@ struct Cluster {
   u64* part;  // [2][MAX_CS][NV]
 
   template <int N, typename Op>
-  __device__ __forceinline__ void fold(u64 (&v)[N], Op op) {
+  __device__ __forceinline__ void fold_block(u64 (&v)[N], Op op) {  // v valid in thread i < N as v[0], for value i
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -101,10 +117,15 @@ struct Cluster {
 #pragma unroll
       for (int i = 0; i < N; ++i) sh[warp * NV + i] = v[i];
     __syncthreads();
-    if ((int)threadIdx.x < N) {
-      u64 r = sh[threadIdx.x];
-      for (int w = 1; w < WARPS; ++w) r = op(r, sh[w * NV + threadIdx.x]);
-      for (int q = 0; q < n; ++q) *cl.map_shared_rank(part + (phase * MAX_CS + rank) * NV + threadIdx.x, q) = r;
+  }
+  template <int N, typename Op>
+  __device__ __forceinline__ void fold(u64 (&v)[N], Op op) {
+    fold_block(v, op);
+    if ((int)threadIdx.x < N * n) {  // one thread per value and CTA that is told
+      const int i = threadIdx.x % N, q = threadIdx.x / N;
+      u64 r = sh[i];
+      for (int w = 1; w < WARPS; ++w) r = op(r, sh[w * NV + i]);
+      *cl.map_shared_rank(part + (phase * MAX_CS + rank) * NV + i, q) = r;
     }
     cl.sync();
 #pragma unroll
@@ -119,18 +140,23 @@ struct Cluster {
   __device__ __forceinline__ void sum(u64 (&v)[N]) {
     fold(v, [](u64 a, u64 b) { return a + b; });
   }
-  __device__ __forceinline__ u64 sum(u64 x) {
-    u64 v[1] = {x};
-    sum(v);
-    return v[0];
-  }
   __device__ __forceinline__ u64 max(u64 x) {
     u64 v[1] = {x};
     fold(v, [](u64 a, u64 b) { return a > b ? a : b; });
     return v[0];
   }
+  template <int N>
+  __device__ __forceinline__ void sum_block(u64 (&v)[N]) {
+    fold_block(v, [](u64 a, u64 b) { return a + b; });
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      u64 r = 0;
+      for (int w = 0; w < WARPS; ++w) r += sh[w * NV + i];
+      v[i] = r;
+    }
+  }
   // What precedes this thread's x in this CTA, and its total
-  __device__ __forceinline__ u64 block_scan(u64 x, u64& total) {
+  __device__ __forceinline__ u64 scan_block(u64 x, u64& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     u64 inc = x;
 #pragma unroll
@@ -143,17 +169,18 @@ struct Cluster {
     __syncthreads();
     u64 before = inc - x;
     total = 0;
+#pragma unroll
     for (int w = 0; w < WARPS; ++w) {
-      if (w < warp) before += sh[w];
-      total += sh[w];
+      const u64 s = sh[w];
+      if (w < warp) before += s;
+      total += s;
     }
     return before;
   }
-  // a[0 .. n) ascending, n <= LIST (a has room for the next power of two)
+  // a[0 .. n) ascending (a has room for the next power of two)
   __device__ __forceinline__ void sort(u64* a, int n) {
     int size = 2;
     while (size < n) size *= 2;
-    __syncthreads();
     for (int i = n + threadIdx.x; i < size; i += THREADS) a[i] = ~0ull;
     __syncthreads();
     for (int k = 2; k <= size; k *= 2)
@@ -169,9 +196,8 @@ struct Cluster {
   // What precedes this thread's x in the order (rank, thread), and the total
   __device__ __forceinline__ u64 scan(u64 x, u64& total) {
     u64 mine;
-    u64 before = block_scan(x, mine);
-    if (threadIdx.x == 0)
-      for (int q = 0; q < n; ++q) *cl.map_shared_rank(part + (phase * MAX_CS + rank) * NV, q) = mine;
+    u64 before = scan_block(x, mine);
+    if ((int)threadIdx.x < n) *cl.map_shared_rank(part + (phase * MAX_CS + rank) * NV, threadIdx.x) = mine;
     cl.sync();
     total = 0;
     for (int q = 0; q < n; ++q) {
@@ -185,355 +211,415 @@ struct Cluster {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(THREADS) sample_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constant__ Params p) {
   extern __shared__ __align__(16) unsigned char smp_smem[];
-  __shared__ double s_table[64];
-  __shared__ u64 s_sh[WARPS * NV], s_part[2 * MAX_CS * NV], s_before[3];
+  __shared__ double s_table[256];
+  __shared__ u64 s_sh[WARPS * NV], s_part[2 * MAX_CS * NV], s_before[3], s_upto, s_cut;
   __shared__ int s_found[3];
-  __shared__ unsigned s_count;
+  __shared__ unsigned s_mine[2], s_sent[2][MAX_CS];  // tokens this CTA has sent, and what every CTA has, for either cut
   cg::cluster_group cl = cg::this_cluster();
   Cluster R{cl, (int)cl.num_blocks(), (int)cl.block_rank(), 0, s_sh, s_part};
   const int tid = threadIdx.x, row = blockIdx.x / R.n, V = p.V;
   const int v_lo = min(V, R.rank * p.per), n = min(V, v_lo + p.per) - v_lo;  // this CTA's tokens
-  if (tid < 64) s_table[tid] = exp2((double)tid / 64);
+  const float temp = p.temperature ? __ldg(p.temperature + row) : 1.f, u = __ldg(p.u + row);
+  const float top_p = p.top_p ? __ldg(p.top_p + row) : 1.f, min_p = p.min_p ? __ldg(p.min_p + row) : 0.f;
+  const int top_k = p.top_k ? __ldg(p.top_k + row) : 0;
 
-  // ---- the slice, 16 bytes at a time but for its ends; an element that is no number counts as masked out ----
-  const T* src = static_cast<const T*>(p.logits) + row * p.ld + v_lo;
+  // ---- the slice, in pieces of 16 bytes as they lie in memory; an element that is no number counts as masked out ----
   constexpr int VEC = 16 / sizeof(T);
+  const T* src = static_cast<const T*>(p.logits) + row * p.ld + v_lo;
   const int head = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));  // elements from the 16-byte boundary before the slice
-  T* z_sm = reinterpret_cast<T*>(smp_smem) + head;                              // z_sm[i]: token v_lo + i
+  const int n_piece = (head + n + VEC - 1) / VEC;
+  uint4* z_sm = reinterpret_cast<uint4*>(smp_smem);  // piece i: tokens v_lo - head + VEC i ..; masked out where they are not this slice's
+  auto unpack = [](const uint4& w, float (&z)[VEC]) {
+    const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) z[j] = to_f32<T>(e[j]);
+  };
   float top = -INFINITY;
-  auto clean = [](float z) { return z == z ? z : -INFINITY; };
   {
-    const int lead = min(n, head ? VEC - head : 0), n_vec = (n - lead) / VEC, tail = lead + n_vec * VEC;
-    for (int i = tid; i < lead + n - tail; i += THREADS) {
-      const int e = i < lead ? i : tail + i - lead;
-      const float z = clean(to_f32<T>(src[e]));
-      z_sm[e] = T(z), top = fmaxf(top, z);
-    }
-    const uint4* vs = reinterpret_cast<const uint4*>(src + lead);
-    uint4* vd = reinterpret_cast<uint4*>(z_sm + lead);
+    const uint4* vs = reinterpret_cast<const uint4*>(src - head);
 #pragma unroll 4
-    for (int i = tid; i < n_vec; i += THREADS) {
-      uint4 w = __ldcs(vs + i);
+    for (int i = tid; i < n_piece; i += THREADS) {
+      const int e0 = i * VEC - head;
+      uint4 w;
       T* e = reinterpret_cast<T*>(&w);
+      if (e0 >= 0 && e0 + VEC <= n) w = __ldcs(vs + i);
+      else
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) e[j] = e0 + j >= 0 && e0 + j < n ? src[e0 + j] : T(-INFINITY);
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const float z = clean(to_f32<T>(e[j]));
-        e[j] = T(z), top = fmaxf(top, z);
+        const float z = to_f32<T>(e[j]);
+        if (z != z) e[j] = T(-INFINITY);
+        top = fmaxf(top, z);  // (of a number and none: the number)
       }
-      vd[i] = w;
+      z_sm[i] = w;
     }
   }
-  auto z_at = [&](int i) { return to_f32<T>(z_sm[i]); };
+  if (tid < 256) s_table[tid] = exp2((double)tid / 256);
+  // f(logits of a piece, token of its first) for this thread's pieces
+  auto each = [&](auto f) {
+#pragma unroll 2
+    for (int i = tid; i < n_piece; i += THREADS) {
+      float z[VEC];
+      unpack(z_sm[i], z);
+      f(z, v_lo - head + i * VEC);
+    }
+  };
   const unsigned top_key = (unsigned)R.max(key_of(top));
-  top = __uint_as_float(top_key & 0x80000000u ? top_key & 0x7fffffffu : ~top_key);
-  const bool writer = R.rank == 0 && tid == 0;
+  top = logit_of(top_key);
   auto put = [&](int token, float prob) {
     p.token[row] = token;
     if (p.prob) p.prob[row] = prob;
   };
+  const bool writer = R.rank == 0 && tid == 0;
   if (top == -INFINITY) {  // nothing to choose from
     if (writer) put(-1, 0.f);
     return;
   }
-  const float temp = p.temperature ? __ldg(p.temperature + row) : 1.f;
   if (!(temp > 0.f)) {  // greedy: the first of the largest
-    u64 first = 0;
-    for (int i = tid; i < n; i += THREADS)
-      if (z_at(i) == top) {
-        first = 0x7fffffffu - (unsigned)(v_lo + i);
-        break;
-      }
-    first = R.max(first);
-    if (writer) put((int)(0x7fffffffu - (unsigned)first), 1.f);
+    unsigned first = 0;
+    each([&](const float (&z)[VEC], int v) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        if (z[j] == top) first = max(first, 0x7fffffffu - (unsigned)(v + j));
+    });
+    first = (unsigned)R.max(first);
+    if (writer) put((int)(0x7fffffffu - first), 1.f);
     return;
   }
-  const Weigher weigh = {s_table, widen(top), 1.4426950408889634074 / (double)temp, p.shift, top == INFINITY ? 3.402823466e38f : -INFINITY};
-  const int top_k = p.top_k ? __ldg(p.top_k + row) : 0;
-  const float top_p = p.top_p ? __ldg(p.top_p + row) : 1.f, min_p = p.min_p ? __ldg(p.min_p + row) : 0.f;
-  const double least = min_p > 0.f ? (double)fminf(min_p, 1.f) * (double)(1ull << p.shift) : 0.0;
-
-  // ---- the cut: a token stays if its key is above `cut`, or equal to it and its index at most `last` ----
-  unsigned cut = 0;
-  int last = V - 1;
-  auto kept = [&](unsigned k, int v) { return k > cut || (k == cut && v <= last); };
-  const int seg = ((n + THREADS - 1) / THREADS) | 1, s_lo = min(n, tid * seg), s_hi = min(n, s_lo + seg);  // (odd: no bank twice)
-  const float u = __ldg(p.u + row);
+  const double log2_t = 1.4426950408889634074 / (double)temp;
+  const Weigher weigh = {s_table, widen(top), 256.0 * log2_t, p.shift, top == INFINITY ? 3.402823466e38f : -INFINITY,
+                         (unsigned)__double2hiint(-256.0 * (p.shift + 2))};
+  const double one = (double)(1ull << p.shift), least = min_p > 0.f ? (double)fminf(min_p, 1.f) * one : 0.0;
   const bool by_k = top_k > 0 && top_k < V, by_p = top_p > 0.f && top_p < 1.f;
+
+  // ---- the cut: tokens of places up to this one stay ----
+  u64 cut = ~0ull;
   if (by_k || by_p) {
-    // Both cuts lie at a place in the ranking, and a histogram over the distance from the best logit says in which bin.  A bin's weights
-    // lie between those of its ends, so it brackets the place of top-p, too.  Mostly few tokens rank that high: they are sent to one CTA,
-    // which sorts them and does the rest alone.  Tokens too far down to weigh anything are in no bin: a cut among them cuts nothing.
-    unsigned* hist = reinterpret_cast<unsigned*>(smp_smem + p.hist_off);
-    u64* list = reinterpret_cast<u64*>(smp_smem + p.hist_off + BINS * 4);
-    const float scale = (float)fmin(BINS / (double)(p.shift + 2) * weigh.c, 1e30);  // (rounded alike for all: the bins are as monotonous as the logits)
-    const double step = weigh.c > 0.0 ? weigh.c / (double)scale : 0.0;             // log2 of the weights' ratio from one end of a bin to the other
-    auto bin_of = [&](float z) -> int {  // BINS: none
+    // A histogram over the distance from the best logit says in which bin a cut lies.  Beside its tokens a bin counts how far down in it they
+    // lie, in 1 / 1024 of its width: by the chord and the tangent of 2^-x that brackets its mass to some 2^-10 of the width's 3 %, so the place
+    // of top-p comes out to within a bin or two.  Tokens too far down to weigh anything are in no bin: a cut among them cuts nothing.
+    unsigned* hist = reinterpret_cast<unsigned*>(smp_smem + p.hist_off);  // [BINS]: tokens, then [BINS]: how far down
+    u64* list = reinterpret_cast<u64*>(hist + 2 * BINS);
+    const float scale = (float)fmin(BINS / (double)(p.shift + 2) * log2_t, 1e30);  // (rounded alike for all: the bins are as monotonous as the logits)
+    const double step = log2_t > 0.0 ? log2_t / (double)scale : 0.0;               // log2 of the weights' ratio from one end of a bin to the other
+    auto depth_of = [&](float z) -> float {  // BINS or more: in no bin
       const float d = (z == top ? 0.f : top - z) * scale;
-      return z > weigh.none && d < (float)BINS ? (int)d : BINS;
+      return z > weigh.none ? d : (float)BINS;
     };
-    for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;
-    if (tid == 0) s_count = 0, s_found[0] = s_found[1] = s_found[2] = BINS;
+    for (int i = tid; i < BINS / 2; i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) s_cut = ~0ull, s_mine[0] = s_mine[1] = 0, s_found[0] = s_found[1] = s_found[2] = BINS;
     __syncthreads();
-    u64 all = 0;
-    for (int i = tid; i < n; i += THREADS) {
-      const float z = z_at(i);
-      const int b = bin_of(z);
-      if (b < BINS) {
-        atomicAdd(hist + b, 1u);
-        if (!by_k) all += weigh(z);
+    each([&](const float (&z)[VEC], int) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float d = depth_of(z[j]);
+        if (d < (float)BINS) {
+          const int b = (int)d;
+          atomicAdd(hist + b, 1u);
+          if (by_p) atomicAdd(hist + BINS + b, (unsigned)((d - (float)b) * 1024.f));
+        }
       }
+    });
+    cl.sync();
+    // this thread's two bins in the whole cluster
+    u64 cnt[2] = {0, 0}, low[2] = {0, 0};
+    {
+      uint2 c[MAX_CS], l[MAX_CS];
+#pragma unroll
+      for (int q = 0; q < MAX_CS; ++q) {
+        const unsigned* h = cl.map_shared_rank(hist, min(q, R.n - 1)) + 2 * tid;
+        c[q] = l[q] = make_uint2(0, 0);
+        if (q < R.n) {
+          c[q] = *reinterpret_cast<const uint2*>(h);
+          if (by_p) l[q] = *reinterpret_cast<const uint2*>(h + BINS);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < MAX_CS; ++q) cnt[0] += c[q].x, cnt[1] += c[q].y, low[0] += l[q].x, low[1] += l[q].y;
     }
-    if (by_k) cl.sync();  // the histograms are complete
-    else all = R.sum(all);
-    // this thread's two bins in the whole cluster, and what lies above them
-    u64 cnt[2] = {0, 0};
-    for (int q = 0; q < R.n; ++q) {
-      const uint2 c = *reinterpret_cast<const uint2*>(cl.map_shared_rank(hist + 2 * tid, q));
-      cnt[0] += c.x, cnt[1] += c.y;
-    }
-    // the first bin at whose end the sum of w[] over the bins reaches target: s_found[slot], the sum before it: s_before[slot]
-    auto crossing = [&](u64 w0, u64 w1, u64 target, int slot) {
-      u64 total;
-      const u64 before = R.block_scan(w0 + w1, total);
+    // the first bin at whose end the sum of w over the bins reaches target: s_found[slot]; the sum before it: s_before[slot]
+    auto crossing = [&](u64 before, u64 w0, u64 w1, u64 target, int slot) {
       if (before < target && target <= before + w0 + w1) {
         const int second = before + w0 < target;
         s_found[slot] = 2 * tid + second, s_before[slot] = before + (second ? w0 : 0);
       }
-      __syncthreads();
     };
-    int b_k = BINS;       // the bin where top-k cuts, and how many of it stay
+    u64 n_all;
+    const u64 n_before = R.scan_block(cnt[0] + cnt[1], n_all);  // tokens of the bins above this thread's
+    int b_k = BINS;      // the bin where top-k cuts, and how many of it stay
     u64 of_b_k = 0;
     if (by_k) {
-      crossing(cnt[0], cnt[1], top_k, 0);
+      crossing(n_before, cnt[0], cnt[1], top_k, 0);
+      __syncthreads();
       b_k = s_found[0];
       if (b_k < BINS) of_b_k = top_k - s_before[0];
     }
-    auto count_to = [&](int b) -> u64 {  // tokens in the bins up to b
-      u64 total;
-      R.block_scan((2 * tid <= b ? cnt[0] : 0) + (2 * tid + 1 <= b ? cnt[1] : 0), total);
-      return total;
-    };
-    // bins between which top-p cuts, given the mass it is to reach
+    // Bins between which top-p cuts.  Weights of a bin of c tokens and summed depths D (in bins; c / 1024 may be missing): with r = 2^-step, at
+    // depth x of it r^x <= 1 - x (1 - r) (chord) and r^x >= 1 + x ln r (tangent), times the weight at the bin's upper end.
     int b_lo = 0, b_hi = BINS - 1;
-    auto bracket = [&](u64 target) {
+    auto bracket = [&]() {
       u64 up[2], down[2];
+      const double r = exp2(-step);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int b = 2 * tid + j;
-        const u64 c = b < b_k ? cnt[j] : b == b_k ? of_b_k : 0;
-        const double one = (double)(1ull << p.shift);
-        up[j] = c * (u64)(exp2(-b * step * (1.0 - 1e-6)) * one * (1.0 + 1e-9) + 1.0);
-        down[j] = c * (u64)(exp2(-(b + 1) * step * (1.0 + 1e-6)) * one * (1.0 - 1e-9));
+        const bool part = b == b_k;  // of the bin where top-k cut only of_b_k tokens are left, whichever
+        const double c = b < b_k ? (double)cnt[j] : part ? (double)of_b_k : 0.0, at = exp2(-b * step) * one;
+        const double d0 = part ? 0.0 : (double)low[j] / 1024, d1 = part ? c : fmin(c, ((double)low[j] + c) / 1024);
+        up[j] = (u64)(at * (c - d0 * (1.0 - r)) * (1.0 + 1e-5) + c);
+        down[j] = (u64)(at * fmax(c + d1 * -0.69314718055994530942 * step, c * r) * (1.0 - 1e-5));  // (1e-5: the roundings of a depth)
+        if (down[j] > (u64)c) down[j] -= (u64)c;  // (weights are rounded)
+        else down[j] = 0;
       }
-      crossing(up[0], up[1], target, 1);
-      crossing(down[0], down[1], target, 2);
+      u64 up_all, down_all;
+      const u64 up_before = R.scan_block(up[0] + up[1], up_all), down_before = R.scan_block(down[0] + down[1], down_all);
+      crossing(up_before, up[0], up[1], times<true>(top_p, down_all), 1);    // the mass may be this small: it is reached here at the earliest
+      crossing(down_before, down[0], down[1], times<true>(top_p, up_all), 2);  // ... or this large
+      __syncthreads();
       b_lo = min(s_found[1], BINS - 1), b_hi = min(s_found[2], min(b_k, BINS - 1));
     };
-    if (!by_k) bracket(times<true>(top_p, all));
+    if (by_p && !by_k) bracket();
+    auto count_to = [&](int b) -> u64 {  // tokens of the bins up to b
+      if (2 * tid == (b & ~1)) s_upto = n_before + cnt[0] + (b & 1 ? cnt[1] : 0);
+      __syncthreads();
+      return s_upto;
+    };
+    // Sends this CTA's tokens of the bins b0 .. b1, in no order, to its part of CTA 0's list, and their number to all; with MASS, also: the exact weight
+    // of what is kept so far, and the part of it in the bins before b0.  Complete after the next barrier of the cluster.
+    u64 sums[2] = {0, 0};
+    const unsigned room = LIST / R.n;
+    auto send = [&](int which, int b0, int b1, auto mass) {
+      u64* to = cl.map_shared_rank(list, 0) + R.rank * room;
+      const float f0 = (float)b0, f1 = (float)(b1 + 1);  // (b1 < BINS)
+      each([&](const float (&z)[VEC], int v) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float d = depth_of(z[j]);
+          if constexpr (mass.value) {
+            u64 w = weigh(z[j]);
+            if (cut != ~0ull && place_of(z[j], v + j) > cut) w = 0;
+            sums[0] += w, sums[1] += d < f0 ? w : 0;
+          }
+          if (d >= f0 && d < f1) {
+            const unsigned at = atomicAdd(s_mine + which, 1u);
+            if (at < room) to[at] = place_of(z[j], v + j);
+          }
+        }
+      });
+      __syncthreads();
+      if (tid < R.n) *cl.map_shared_rank(&s_sent[which][R.rank], tid) = s_mine[which];
+    };
+    // CTA 0 closes the gaps in its list (all its threads call); the tokens in it
+    auto collect = [&](int which) -> int {
+      u64 e[LIST / THREADS];
+      int at[LIST / THREADS], all = 0;
+#pragma unroll
+      for (int j = 0; j < LIST / THREADS; ++j) {
+        const int i = tid + j * THREADS, q = i / (int)room, k = i - q * (int)room;
+        e[j] = list[i], at[j] = -1;
+        if (q < R.n && k < (int)s_sent[which][q]) {
+          at[j] = k;
+          for (int x = 0; x < q; ++x) at[j] += s_sent[which][x];
+        }
+      }
+      for (int q = 0; q < R.n; ++q) all += s_sent[which][q];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < LIST / THREADS; ++j)
+        if (at[j] >= 0) list[at[j]] = e[j];
+      __syncthreads();
+      return all;
+    };
+    // Up to SOLO tokens in the list: a group of threads for each goes over all others.  This thread's token, its number in the list (SOLO and more:
+    // none), the number of its group's threads that are ahead of it
+    u64* weights = list + LIST;
+    struct Mine {
+      u64 place;
+      int at, part, lanes;
+    };
+    auto mine_of = [&](int N) -> Mine {
+      int lanes = 32;
+      while (lanes * N > THREADS) lanes >>= 1;
+      const int at = tid / lanes;
+      return {at < N ? list[at] : ~0ull, at, tid & (lanes - 1), lanes};
+    };
+    // sum of the weights, and the number, of the tokens for which the test holds
+    auto over_others = [&](const Mine& m, int N, auto test, u64& sum, int& count) {
+      sum = 0, count = 0;
+      for (int i = m.part; i < N; i += m.lanes)
+        if (test(list[i])) sum += weights[i], ++count;
+      for (int o = m.lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o), count += __shfl_xor_sync(0xffffffffu, count, o);
+    };
     const int b_end = by_k ? min(b_k, BINS - 1) : b_hi;
-    const u64 n_list = count_to(b_end);
-
-    if (n_list <= LIST) {
-      // ---- the candidates go to CTA 0 ----
-      u64* far = cl.map_shared_rank(list, 0);
-      unsigned* counter = cl.map_shared_rank(&s_count, 0);
-      for (int i0 = 0; i0 < n; i0 += THREADS) {
-        const int i = i0 + tid;
-        const float z = i < n ? z_at(i) : -INFINITY;
-        const bool in = i < n && bin_of(z) <= b_end;
-        const unsigned who = __ballot_sync(0xffffffffu, in);
-        if (who == 0) continue;
-        unsigned at = 0;
-        if ((tid & 31) == 0) at = atomicAdd(counter, (unsigned)__popc(who));
-        at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << (tid & 31)) - 1));
-        if (in) far[at] = (u64)~key_of(z) << 32 | (unsigned)(v_lo + i);
+    const u64 n_cand = count_to(b_end);
+    if (n_cand <= SOLO) {
+      // ---- few candidates: CTA 0 does the rest with a group of threads for each, which goes over all others ----
+      if (by_p && !by_k) {
+        send(0, 0, b_end, std::true_type{});
+        R.sum(sums);
+      } else {
+        send(0, 0, b_end, std::false_type{});
+        cl.sync();
       }
-      cl.sync();
       if (R.rank != 0) return;
-      const int N = (int)n_list;
-      R.sort(list, N);
-      // rank j of the list: thread j / 4
-      constexpr int PER = LIST / THREADS;
-      auto z_of = [](unsigned key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); };
-      u64 w[PER], sum = 0, total;
-      double wd[PER];
-      const int limit = by_k ? min(N, top_k) : N;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const int at = tid * PER + j;
-        wd[j] = at < limit ? weigh.scaled(z_of(~(unsigned)(list[at] >> 32))) : 0.0;
-        w[j] = weigh.rounded(wd[j]), sum += w[j];
-      }
-      u64 before = R.block_scan(sum, total);
-      const u64 target = by_p ? (by_k ? times<true>(top_p, total) : times<true>(top_p, all)) : ~0ull;
-      int stay = 0;  // of this thread's: those before the target is reached and not below min-p (a prefix of the ranking)
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        stay += tid * PER + j < limit && before < target && w[j] > 0 && wd[j] >= least;
-        before += w[j];
-      }
-      u64 n_kept;
-      R.block_scan(stay, n_kept);
-      // the kept ones by index
-      u64 mine[PER];
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const u64 e = tid * PER + j < N ? list[tid * PER + j] : 0;
-        mine[j] = e << 32 | e >> 32;
-      }
+      const int N = collect(0);
+      const Mine m = mine_of(N);
+      const bool first = m.at < N && m.part == 0;
+      const double wd = m.at < N ? weigh.scaled(logit_at(m.place)) : 0.0;
+      const u64 w = Weigher::rounded(wd);
+      if (first) weights[m.at] = w;
       __syncthreads();
-#pragma unroll
-      for (int j = 0; j < PER; ++j)
-        if (tid * PER + j < (int)n_kept) list[tid * PER + j] = mine[j];
+      u64 before;
+      int rank;
+      over_others(m, N, [&](u64 x) { return x < m.place; }, before, rank);
+      u64 s[1] = {0};
+      const bool in_k = m.at < N && (!by_k || rank < top_k);
+      u64 target = ~0ull;
+      if (by_p) {
+        if (by_k) {
+          s[0] = first && in_k ? w : 0;
+          R.sum_block(s);
+          target = times<true>(top_p, s[0]);
+        } else {
+          target = times<true>(top_p, sums[0]);
+        }
+      }
+      const bool stays = in_k && before < target && wd >= least;
       __syncthreads();
-      R.sort(list, (int)n_kept);
-      sum = 0;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        const int at = tid * PER + j;
-        wd[j] = at < (int)n_kept ? weigh.scaled(z_of(~(unsigned)list[at])) : 0.0;
-        w[j] = weigh.rounded(wd[j]), sum += w[j];
-      }
-      before = R.block_scan(sum, total);
-      const u64 at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) {
-        if (before <= at && at < before + w[j]) put((int)(list[tid * PER + j] >> 32), (float)(wd[j] / (double)total));
-        before += w[j];
-      }
+      if (first && !stays) weights[m.at] = 0;
+      s[0] = first && stays ? w : 0;
+      R.sum_block(s);
+      const u64 total = s[0], at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;
+      over_others(m, N, [&](u64 x) { return token_at(x) < token_at(m.place); }, before, rank);
+      if (first && stays && before <= at && at < before + w) put(token_at(m.place), (float)(wd / (double)total));
       return;
     }
 
-    // ---- many tokens stay: the cuts are found by all CTAs together ----
-    // this CTA's tokens of the bins b0 .. b1, listed where they fit (all CTAs decide alike)
-    bool listed = false;
-    unsigned n_mine = 0;
-    auto gather = [&](int b0, int b1) {
-      __syncthreads();
-      if (tid == 0) s_count = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += THREADS) {
-        const float z = z_at(i);
-        const int b = bin_of(z);
-        if (b < b0 || b > b1) continue;
-        const unsigned at = atomicAdd(&s_count, 1u);
-        if (at < LIST) list[at] = (u64)key_of(z) << 32 | (unsigned)(v_lo + i);
-      }
-      __syncthreads();
-      n_mine = s_count;
-      listed = R.max(n_mine) <= LIST;
-    };
-    auto each = [&](int b0, int b1, auto f) {  // f(key, logit, token) for this thread's tokens of the gathered bins
-      if (listed) {
-        for (unsigned i = tid; i < n_mine; i += THREADS) {
-          const unsigned key = (unsigned)(list[i] >> 32);
-          f(key, __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key), (int)(unsigned)list[i]);
-        }
-      } else {
-        for (int i = tid; i < n; i += THREADS) {
-          const float z = z_at(i);
-          const int b = bin_of(z);
-          if (b >= b0 && b <= b1) f(key_of(z), z, v_lo + i);
-        }
-      }
-    };
-    // index of the need-th token (from 1) of key c, by index
-    auto nth_of_key = [&](unsigned c, u64 need) -> int {
-      u64 mine = 0, total;
-      for (int i = s_lo; i < s_hi; ++i) mine += key_of(z_at(i)) == c;
-      u64 before = R.scan(mine, total);
-      u64 at = 0;
-      if (before < need && need <= before + mine)
-        for (int i = s_lo; i < s_hi; ++i)
-          if (key_of(z_at(i)) == c && ++before == need) at = v_lo + i;
-      return (int)R.max(at);
-    };
-    // largest key c such that the sum of val(key, logit, token) over the gathered tokens of key >= c reaches `target` (three bits a pass)
-    auto search = [&](int b0, int b1, auto val, u64 target) -> unsigned {
-      unsigned c = 0;
-      for (int shift = 30; shift >= 0; shift -= 3) {
+    // ---- many tokens stay: only those of the bins where a cut lies are sent ----
+    // The smallest place c such that the sum of val(logit, place) over the places up to c reaches target, among all CTAs' tokens of the bins b0 ..
+    // b1: three bits of it a pass.  For lists that do not fit (many equal logits).
+    auto search = [&](int b0, int b1, auto val, u64 target) -> u64 {
+      u64 c = 0, base = 0;
+      for (int shift = 48; shift >= 0; shift -= 3) {
         u64 s[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) s[k] = 0;
-        each(b0, b1, [&](unsigned key, float z, int v) {
-          if (key < (c | (1u << shift))) return;
-          const u64 x = val(key, z, v);
+        each([&](const float (&z)[VEC], int v) {
 #pragma unroll
-          for (int k = 0; k < NV; ++k) {
-            const u64 cand = c + ((u64)(k + 1) << shift);  // (beyond 32 bits in the first pass: never reached)
-            if (key >= cand) s[k] += x;
+          for (int j = 0; j < VEC; ++j) {
+            const float d = depth_of(z[j]);
+            const u64 place = place_of(z[j], v + j);
+            if (!(d >= (float)b0 && d < (float)(b1 + 1)) || place >> (shift + 3) != c >> (shift + 3)) continue;
+            const u64 x = val(z[j], place);
+            const int digit = (int)(place >> shift) & 7;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) s[k] += digit <= k ? x : 0;
           }
         });
         R.sum(s);
-        unsigned best = 0;
+        int digit = NV;
+#pragma unroll
+        for (int k = NV - 1; k >= 0; --k)
+          if (base + s[k] >= target) digit = k;
+        u64 skipped = 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-          if (c + ((u64)(k + 1) << shift) <= 0xffffffffull && s[k] >= target) best = k + 1;
-        c += best << shift;
+          if (k + 1 == digit) skipped = s[k];
+        base += skipped, c |= (u64)digit << shift;
       }
       return c;
     };
+    // The same among the tokens sent (the barrier that completes them is passed), by CTA 0, which tells the others
+    auto find = [&](int which, int b0, int b1, auto val, u64 target) -> u64 {
+      unsigned most = 0;
+      for (int q = 0; q < R.n; ++q) most = max(most, s_sent[which][q]);
+      if (most > room) return search(b0, b1, val, target);
+      if (R.rank == 0) {
+        const int N = collect(which);
+        auto tell = [&](u64 c) {
+          for (int q = 0; q < R.n; ++q) *cl.map_shared_rank(&s_cut, q) = c;
+        };
+        if (N <= SOLO) {
+          const Mine m = mine_of(N);
+          const bool first = m.at < N && m.part == 0;
+          const u64 w = m.at < N ? val(logit_at(m.place), m.place) : 0;
+          if (first) weights[m.at] = w;
+          __syncthreads();
+          u64 before;
+          int rank;
+          over_others(m, N, [&](u64 x) { return x < m.place; }, before, rank);
+          if (first && before < target && target <= before + w) tell(m.place);
+        } else {
+          R.sort(list, N);
+          constexpr int PER = LIST / THREADS;
+          u64 w[PER], sum = 0, total;
+#pragma unroll
+          for (int j = 0; j < PER; ++j) {
+            const int i = tid * PER + j;
+            w[j] = i < N ? val(logit_at(list[i]), list[i]) : 0, sum += w[j];
+          }
+          u64 before = R.scan_block(sum, total);
+#pragma unroll
+          for (int j = 0; j < PER; ++j) {
+            if (before < target && target <= before + w[j]) tell(list[tid * PER + j]);
+            before += w[j];
+          }
+        }
+      }
+      cl.sync();
+      return s_cut;
+    };
     if (b_k < BINS) {
-      gather(b_k, b_k);
-      const unsigned c = search(b_k, b_k, [](unsigned, float, int) -> u64 { return 1; }, of_b_k);
-      u64 s[2] = {0, 0};
-      each(b_k, b_k, [&](unsigned key, float, int) { s[0] += key > c, s[1] += key == c; });
-      R.sum(s);
-      const u64 need = of_b_k - s[0];
-      cut = c;
-      if (need < s[1]) last = nth_of_key(c, need);
+      send(0, b_k, b_k, std::false_type{});
+      cl.sync();
+      cut = find(0, b_k, b_k, [](float, u64) -> u64 { return 1; }, of_b_k);
     }
     if (by_p) {
-      auto mass = [&](unsigned key, float z, int v) -> u64 { return kept(key, v) ? weigh(z) : 0; };
-      if (by_k) {
-        all = 0;
-        for (int i = tid; i < n; i += THREADS) all += mass(key_of(z_at(i)), z_at(i), v_lo + i);
-        all = R.sum(all);
-        bracket(times<true>(top_p, all));
-      }
-      u64 above = 0;
-      for (int i = tid; i < n; i += THREADS) {
-        const float z = z_at(i);
-        if (bin_of(z) < b_lo) above += weigh(z);
-      }
-      const u64 target = times<true>(top_p, all) - R.sum(above);
-      gather(b_lo, b_hi);
-      const unsigned c = search(b_lo, b_hi, mass, target);
-      u64 s[3] = {0, 0, 0};  // mass above c, tokens of key c, their weight
-      each(b_lo, b_hi, [&](unsigned key, float z, int v) {
-        if (key > c) s[0] += mass(key, z, v);
-        else if (key == c) s[1] += 1, s[2] += weigh(z);
-      });
-      R.sum(s);
-      const u64 one = s[2] / s[1], need = (target - s[0] + one - 1) / one;
-      if (c > cut) last = V - 1;
-      if (need < s[1]) last = min(last, nth_of_key(c, need));  // (at the key where top-k cut, need stays within what it kept)
-      cut = c;
+      if (by_k) bracket();
+      send(1, b_lo, b_hi, std::true_type{});
+      R.sum(sums);
+      const u64 c = find(1, b_lo, b_hi, [&](float z, u64 place) -> u64 { return place <= cut ? weigh(z) : 0; }, times<true>(top_p, sums[0]) - sums[1]);
+      cut = c < cut ? c : cut;
     }
   }
 
-  // ---- the draw: every thread has a run of neighbouring tokens ----
-  auto weight = [&](int i) -> double {
-    const float z = z_at(i);
-    if (!kept(key_of(z), v_lo + i)) return 0.0;
+  // ---- the draw: every thread has a run of neighbouring pieces ----
+  auto weight = [&](float z, int v) -> double {
     const double w = weigh.scaled(z);
-    return w >= least ? w : 0.0;
+    return w >= least && place_of(z, v) <= cut ? w : 0.0;
   };
+  const int run = ((n_piece + THREADS - 1) / THREADS) | 1, r_lo = min(n_piece, tid * run), r_hi = min(n_piece, r_lo + run);  // (odd: no bank twice)
   u64 mine = 0, total;
-  for (int i = s_lo; i < s_hi; ++i) mine += weigh.rounded(weight(i));
+  auto add_up = [&](auto all) {
+    for (int i = r_lo; i < r_hi; ++i) {
+      float z[VEC];
+      unpack(z_sm[i], z);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        if constexpr (all.value) mine += weigh(z[j]);
+        else mine += Weigher::rounded(weight(z[j], v_lo - head + i * VEC + j));
+      }
+    }
+  };
+  if (cut == ~0ull && least == 0.0) add_up(std::true_type{});
+  else add_up(std::false_type{});
   u64 before = R.scan(mine, total);
   const u64 at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;  // (total is 2^S at least: the largest logit stays)
-  if (before <= at && at < before + mine)
-    for (int i = s_lo; i < s_hi; ++i) {
-      const double w = weight(i);
-      before += weigh.rounded(w);
+  if (before <= at && at < before + mine) {
+    const T* zs = reinterpret_cast<const T*>(z_sm);
+    for (int e = r_lo * VEC; e < r_hi * VEC; ++e) {
+      const int v = v_lo - head + e;
+      const double w = weight(to_f32<T>(zs[e]), v);
+      before += Weigher::rounded(w);
       if (before > at) {
-        put(v_lo + i, (float)(w / (double)total));
+        put(v, (float)(w / (double)total));
         break;
       }
     }
+  }
 }
 
 }  // namespace smp

@@ -128,10 +128,13 @@ constexpr int SMP_MAX_VOCAB = 1 << 18, SMP_SMEM = 200 * 1024;
 template <typename T>
 int smp_launch(smp::Params& p, void* stream) {
   static std::atomic<unsigned long long> allowed;
-  int cs = p.V >= 16384 ? 8 : p.V >= 4096 ? 4 : 1;
+  constexpr int extra = 32 + smp::BINS * 8 + (smp::LIST + smp::SOLO) * 8;
+  // CTAs per row: as many as the rows leave SMs for (two CTAs share one), none with less than 2048 tokens; more where a slice would not let two CTAs share
+  int cs = 1;
+  while (cs < smp::MAX_CS && ((p.V > 2048 * cs && p.rows * cs <= kSms) || (p.V / cs) * (int)sizeof(T) + extra > 110 * 1024)) cs *= 2;
   p.per = ((p.V + cs - 1) / cs + 7) / 8 * 8;
-  p.hist_off = (p.per * (int)sizeof(T) + 16 + 15) / 16 * 16;
-  const int bytes = p.hist_off + smp::BINS * 4 + smp::LIST * 8;
+  p.hist_off = p.per * (int)sizeof(T) + 32;  // (a piece more than the slice: it need not begin on a boundary)
+  const int bytes = p.hist_off - 32 + extra;
   if (!allow_smem((const void*)smp::sample_kernel<T>, SMP_SMEM, allowed)) return LOOPSPEC_ECUDA;
   return launch(smp::sample_kernel<T>, dim3(p.rows * cs), smp::THREADS, bytes, stream, p, false, cs);
 }
