@@ -4,6 +4,7 @@
 //
 //   prefix_rows_kernel     problems of few rows against many keys: a sequence's own keys (its new rows x the query heads of a kv head), and
 //                          the prefix where the whole batch has few rows.  Bound by the stream of keys and values.
+//   prefix_tc_kernel       the prefix against the rows of a larger batch, on tcgen05 (op_prefix_tc.cuh).
 //   prefix_merge_kernel    folds a row's parts in a fixed order, writes it and its log-sum-exp.
 //
 // Scores are bf16 / fp16 products summed in fp32; maximum, sum and weighted values are fp32.  The softmax weights are rounded to the cache's
@@ -36,6 +37,8 @@ struct PrefixParams {
   int* plan;               // [2 NP + 2]: units before problem i, row tiles before it (the last entries: their totals)
   float *item_o, *item_ml; // partials of the tiles whose first key is in the segment: [kv head][row tile][16][D], ..[2]
   float *warp_o, *warp_ml; // partials of the segments that begin inside a tile's keys: [warp][16][D], ..[2]
+  int tc_tiles, tc_splits; // prefix_tc_kernel: tiles of 128 rows, parts of the prefix (0: it does not run)
+  float *tc_o, *tc_ml;     // its partials: [kv head][row tile][part][128][D], ..[2]
   void* out;
   long long out_ld;
   float* lse;              // [T][nq] or null
@@ -161,7 +164,11 @@ __global__ void __launch_bounds__(PXR_WARPS * 32, 2) prefix_rows_kernel(const __
   const long long U = (long long)Us * p.kv.n_kv;
   const int w = blockIdx.x * PXR_WARPS + warp;
   const int W = px_warps(p, U);
-  if (w >= W) return;
+  // (every thread waits before it ends: this kernel may run beside prefix_tc_kernel, and the merge waits for this one only)
+  if (w >= W) {
+    pdl_wait();
+    return;
+  }
   const long long u_lo = w * U / W, u_hi = (w + 1) * U / W;
 
   // a place on the line
@@ -395,6 +402,7 @@ __global__ void __launch_bounds__(PXR_WARPS * 32, 2) prefix_rows_kernel(const __
     }
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");  // (only empty groups are left)
+  pdl_wait();
 }
 
 // One warp per (row, query head): the parts of the prefix and of the sequence's own keys in a fixed order.
@@ -428,13 +436,12 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
     float m = -INFINITY, l = 0.f, acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    for (int which = p.prefix_rows ? 0 : 1; which < 2; ++which) {
-      const int rr = which ? r : row * p.G + (r - j * p.G);  // the row's number within the problem
-      const Part q = part_of(which ? i_own : 0, which ? own.len : p.prefix_len, rr >> 4);
-      for (int x0 = 0; x0 < q.n; x0 += 32) {
-        const int cnt = min(32, q.n - x0), x = x0 + lane;
+    // parts of a problem: count of them, and where part x has its row of weighted values and its (maximum, sum)
+    auto fold = [&](int count, auto o_at, auto ml_at) {
+      for (int x0 = 0; x0 < count; x0 += 32) {
+        const int cnt = min(32, count - x0);
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (lane < cnt) ml = __ldcg(reinterpret_cast<const float2*>((x == 0 ? p.item_ml + q.item * 32 : p.warp_ml + (long long)(q.w0 + x) * 32) + (rr & 15) * 2));
+        if (lane < cnt) ml = __ldcg(reinterpret_cast<const float2*>(ml_at(x0 + lane)));
         const float mx = fmaxf(m, warp_max(ml.x)), ref = mx == -INFINITY ? 0.f : mx;
         const float wt = px_exp2(ml.x - ref), keep = px_exp2(m - ref);
         m = mx;
@@ -444,7 +451,7 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
 #pragma unroll 4
         for (int y = 0; y < cnt; ++y) {
           const float f = __shfl_sync(0xffffffffu, wt, y);
-          const float* src = (x0 + y == 0 ? p.item_o + q.item * 16 * D : p.warp_o + (long long)(q.w0 + x0 + y) * 16 * D) + (rr & 15) * D + lane * V;
+          const float* src = o_at(x0 + y) + lane * V;
           float v[V];
           if constexpr (V == 4) {
             const float4 z = __ldcg(reinterpret_cast<const float4*>(src));
@@ -457,6 +464,17 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
           for (int e = 0; e < V; ++e) acc[e] = fmaf(f, v[e], acc[e]);
         }
       }
+    };
+    const int pr = row * p.G + (r - j * p.G);  // the row's number in the prefix problem
+    if (p.tc_splits) {
+      const long long slot = (long long)(h * p.tc_tiles + (pr >> 7)) * p.tc_splits * 128 + (pr & 127);
+      fold(p.tc_splits, [&](int x) { return p.tc_o + (slot + x * 128) * D; }, [&](int x) { return p.tc_ml + (slot + x * 128) * 2; });
+    }
+    for (int which = p.prefix_rows ? 0 : 1; which < 2; ++which) {
+      const int rr = which ? r : pr;
+      const Part q = part_of(which ? i_own : 0, which ? own.len : p.prefix_len, rr >> 4);
+      fold(q.n, [&](int x) { return (x == 0 ? p.item_o + q.item * 16 * D : p.warp_o + (long long)(q.w0 + x) * 16 * D) + (rr & 15) * D; },
+           [&](int x) { return (x == 0 ? p.item_ml + q.item * 32 : p.warp_ml + (long long)(q.w0 + x) * 32) + (rr & 15) * 2; });
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees no key: zeros
     T* dst = static_cast<T*>(p.out) + (long long)row * p.out_ld + head * D + lane * V;

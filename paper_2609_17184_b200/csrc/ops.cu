@@ -9,6 +9,7 @@
 
 #include "op_append.cuh"
 #include "op_attention.cuh"
+#include "op_prefix_tc.cuh"
 #include "op_sample.cuh"
 
 using namespace ls;
@@ -88,16 +89,30 @@ bool allow_smem(const void* fn, int bytes, std::atomic<unsigned long long>& done
 
 // ---- attention behind a shared prefix ----
 struct PxPlan {
-  int n_warps, max_tiles, prefix_rows;
-  size_t plan_off, item_ml, item_o, warp_ml, warp_o, total;
+  int n_warps, max_tiles, tc_tiles, tc_splits;
+  size_t plan_off, item_ml, item_o, warp_ml, warp_o, tc_ml, tc_o, total;
 };
+constexpr int PXT_MIN_ROWS = 33;  // rows of the batch and a kv head from which on the prefix goes to prefix_tc_kernel
 bool px_plan(int T, int B, int nq, int nkv, int d, int P, PxPlan* o) {
   if (T < 0 || B < 0 || B > PXR_MAX_SEQS || nq < 1 || nkv < 1 || nq % nkv || (d != 64 && d != 128) || P < 0) return false;
   if ((int64_t)T * nq > (1 << 27) || nkv > 65535) return false;
   const int G = nq / nkv, rows = T * G;
-  o->prefix_rows = P > 0;
   o->n_warps = kSms * 2 * PXR_WARPS;
-  o->max_tiles = rows / 16 + B + (o->prefix_rows ? rows / 16 + 1 : 0);
+  o->max_tiles = rows / 16 + B + (P > 0 ? rows / 16 + 1 : 0);
+  o->tc_tiles = o->tc_splits = 0;
+  if (rows >= PXT_MIN_ROWS && P > 0) {
+    // Parts of the prefix: whole rounds of the SMs against the fixed cost of a part (some four tiles' time: queries, first keys, last weights) and
+    // what its partials cost to write and fold.
+    o->tc_tiles = (rows + PXT_ROWS - 1) / PXT_ROWS;
+    const int all = (P + PXT_KEYS - 1) / PXT_KEYS;
+    const int64_t base = (int64_t)o->tc_tiles * nkv;
+    const double per_part = (double)rows * nkv * d * 8 / 8e12 / 0.7e-6;
+    double best = 1e30;
+    for (int s = 1; s <= all && s <= 64; ++s) {
+      const double cost = (double)((base * s + kSms - 1) / kSms) * ((all + s - 1) / s + 4) + s * per_part;
+      if (cost < best) best = cost, o->tc_splits = s;
+    }
+  }
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t r = at;
@@ -109,15 +124,57 @@ bool px_plan(int T, int B, int nq, int nkv, int d, int P, PxPlan* o) {
   o->item_o = take((size_t)nkv * o->max_tiles * 16 * d * 4);
   o->warp_ml = take((size_t)o->n_warps * 128);
   o->warp_o = take((size_t)o->n_warps * 16 * d * 4);
+  const size_t slots = (size_t)nkv * o->tc_tiles * o->tc_splits * PXT_ROWS;
+  o->tc_ml = take(slots * 8);
+  o->tc_o = take(slots * d * 4);
   o->total = at;
   return true;
 }
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+  static std::atomic<EncodeTiledFn> fn;
+  EncodeTiledFn f = fn.load(std::memory_order_acquire);
+  if (!f) {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      return nullptr;
+    }
+    f = reinterpret_cast<EncodeTiledFn>(ptr);
+    fn.store(f, std::memory_order_release);
+  }
+  return f;
+}
+// keys or values as (element, slot, head, page); boxes of 64 elements of `box` slots
+bool cache_map(CUtensorMap* map, const PagedKv& kv, const void* ptr, int dtype, int box) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[4] = {(cuuint64_t)kv.d, (cuuint64_t)1 << kv.page_shift, (cuuint64_t)kv.n_kv, (cuuint64_t)kv.n_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)kv.slot_stride * 2, (cuuint64_t)kv.head_stride * 2, (cuuint64_t)kv.page_stride * 2};
+  cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1}, estr[4] = {1, 1, 1, 1};
+  return fn(map, dtype == 1 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(ptr), dims, strides, boxes, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int D>
-int px_launch(PrefixParams& p, void* stream) {
-  static std::atomic<unsigned long long> allowed;
-  const int NP = p.B + p.prefix_rows;
+int px_launch(PrefixParams& p, const PxPlan& t, int dtype, void* stream) {
+  static std::atomic<unsigned long long> allowed, allowed_tc;
   if (!allow_smem((const void*)prefix_rows_kernel<T, D>, px_rows_smem(D, PXR_MAX_SEQS + 1), allowed)) return LOOPSPEC_ECUDA;
-  const int rc = launch(prefix_rows_kernel<T, D>, dim3(kSms * 2), PXR_WARPS * 32, px_rows_smem(D, NP), stream, p);
+  // The prefix on tcgen05: boxes of at least 8 slots (a swizzled group of rows), strides a tensor map takes; else the rows' kernel has it too.
+  CUtensorMap mk, mv;
+  const int page = 1 << p.kv.page_shift, box = std::min(page, PXT_KEYS);
+  const bool tc = t.tc_splits && page >= 8 && cache_map(&mk, p.kv, p.kv.k, dtype, box) && cache_map(&mv, p.kv, p.kv.v, dtype, box);
+  p.prefix_rows = p.prefix_len > 0 && !tc;
+  if (tc) {
+    p.tc_tiles = t.tc_tiles, p.tc_splits = t.tc_splits;
+    if (!allow_smem((const void*)prefix_tc_kernel<T, D>, pxt_smem(D), allowed_tc)) return LOOPSPEC_ECUDA;
+    prefix_tc_kernel<T, D><<<t.tc_tiles * t.tc_splits * p.kv.n_kv, PXT_THREADS, pxt_smem(D), static_cast<cudaStream_t>(stream)>>>(mk, mv, p);
+    if (cudaGetLastError() != cudaSuccess) return LOOPSPEC_ECUDA;
+  }
+  const int rc = launch(prefix_rows_kernel<T, D>, dim3(kSms * 2), PXR_WARPS * 32, px_rows_smem(D, p.B + p.prefix_rows), stream, p, tc);
   if (rc) return rc;
   const int z = std::max(1, std::min(16, (int)(((int64_t)p.T * p.G / p.B + 3) / 4)));
   return launch(prefix_merge_kernel<T, D>, dim3(p.kv.n_kv, p.B, z), 128, 0, stream, p, true);
@@ -192,7 +249,7 @@ int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t
   const double units = ((double)T * p.G / 16 + n_seqs) * ((double)table_width * kv->page_size / 16 + 1) + ((double)T * p.G / 16 + 1) * ((double)prefix_len / 16 + 1);
   if (units >= 2147483648.0) return LOOPSPEC_EINVAL;
   if (!scratch || scratch_bytes < t.total || (reinterpret_cast<uintptr_t>(scratch) & 255)) return LOOPSPEC_ECAPACITY;
-  p.q = q, p.q_ld = q_ld, p.prefix_pages = prefix_pages, p.prefix_len = prefix_len, p.prefix_rows = t.prefix_rows;
+  p.q = q, p.q_ld = q_ld, p.prefix_pages = prefix_pages, p.prefix_len = prefix_len;
   p.page_table = page_table, p.table_ld = table_ld, p.table_w = table_width, p.lens = lens, p.cu_rows = cu_rows;
   p.B = n_seqs, p.T = T, p.nq = n_q_heads;
   p.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)p.kv.d) : scale) * 1.4426950408889634f;
@@ -201,9 +258,10 @@ int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t
   p.plan = reinterpret_cast<int*>(sc + t.plan_off);
   p.item_ml = reinterpret_cast<float*>(sc + t.item_ml), p.item_o = reinterpret_cast<float*>(sc + t.item_o);
   p.warp_ml = reinterpret_cast<float*>(sc + t.warp_ml), p.warp_o = reinterpret_cast<float*>(sc + t.warp_o);
+  p.tc_ml = reinterpret_cast<float*>(sc + t.tc_ml), p.tc_o = reinterpret_cast<float*>(sc + t.tc_o);
   p.out = out, p.out_ld = out_ld, p.lse = lse, p.flag = flag;
-  if (p.kv.d == 128) return kv->dtype == 1 ? px_launch<__nv_bfloat16, 128>(p, cuda_stream) : px_launch<__half, 128>(p, cuda_stream);
-  return kv->dtype == 1 ? px_launch<__nv_bfloat16, 64>(p, cuda_stream) : px_launch<__half, 64>(p, cuda_stream);
+  if (p.kv.d == 128) return kv->dtype == 1 ? px_launch<__nv_bfloat16, 128>(p, t, 1, cuda_stream) : px_launch<__half, 128>(p, t, 2, cuda_stream);
+  return kv->dtype == 1 ? px_launch<__nv_bfloat16, 64>(p, t, 1, cuda_stream) : px_launch<__half, 64>(p, t, 2, cuda_stream);
 }
 
 int loopspec_op_sample(const void* logits, int32_t dtype, int64_t ld, int32_t rows, int32_t vocab, const float* uniforms, const float* temperature,
