@@ -8,8 +8,7 @@
 #include <cstring>
 
 #include "op_append.cuh"
-#include "op_attention.cuh"
-#include "op_prefix_tc.cuh"
+#include "op_prefix.cuh"
 #include "op_sample.cuh"
 
 using namespace ls;
@@ -73,12 +72,18 @@ AppendFn append_fn(int dtype, int lh) {
 
 constexpr int kSms = 148;
 
-// Lets a kernel ask for `bytes` of dynamic shared memory; `done` remembers, a bit per device, that it may
-bool allow_smem(const void* fn, int bytes, std::atomic<unsigned long long>& done) {
+// Lets a kernel ask for `bytes` of dynamic shared memory; `done` remembers, a bit per device, that it may.  regs: registers a thread that it must have
+// been compiled to (0: any)
+bool allow_smem(const void* fn, int bytes, std::atomic<unsigned long long>& done, int regs = 0) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
   const unsigned long long bit = 1ull << (dev & 63);
   if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+  cudaFuncAttributes a;
+  if (regs && (cudaFuncGetAttributes(&a, fn) != cudaSuccess || a.numRegs != regs)) {
+    (void)cudaGetLastError();
+    return false;
+  }
   if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
     (void)cudaGetLastError();
     return false;
@@ -89,44 +94,30 @@ bool allow_smem(const void* fn, int bytes, std::atomic<unsigned long long>& done
 
 // ---- attention behind a shared prefix ----
 struct PxPlan {
-  int n_warps, max_tiles, tc_tiles, tc_splits;
-  size_t plan_off, item_ml, item_o, warp_ml, warp_o, tc_ml, tc_o, total;
+  int max_tiles, tc_tiles;
+  size_t plan_off, item_ml, item_o, warp_ml, warp_o, tc_item_ml, tc_item_o, tc_work_ml, tc_work_o, total;
 };
-constexpr int PXT_MIN_ROWS = 33;  // rows of the batch and a kv head from which on the prefix goes to prefix_tc_kernel
+constexpr int PXT_MIN_ROWS = 33;  // rows of the batch and a kv head from which on the prefix goes to the tensor cores' tiles
 bool px_plan(int T, int B, int nq, int nkv, int d, int P, PxPlan* o) {
-  if (T < 0 || B < 0 || B > PXR_MAX_SEQS || nq < 1 || nkv < 1 || nq % nkv || (d != 64 && d != 128) || P < 0) return false;
+  if (T < 0 || B < 0 || B > PX_MAX_SEQS || nq < 1 || nkv < 1 || nq % nkv || (d != 64 && d != 128) || P < 0) return false;
   if ((int64_t)T * nq > (1 << 27) || nkv > 65535) return false;
-  const int G = nq / nkv, rows = T * G;
-  o->n_warps = kSms * 2 * PXR_WARPS;
+  const int rows = T * (nq / nkv);
   o->max_tiles = rows / 16 + B + (P > 0 ? rows / 16 + 1 : 0);
-  o->tc_tiles = o->tc_splits = 0;
-  if (rows >= PXT_MIN_ROWS && P > 0) {
-    // Parts of the prefix: whole rounds of the SMs against the fixed cost of a part (some four tiles' time: queries, first keys, last weights) and
-    // what its partials cost to write and fold.
-    o->tc_tiles = (rows + PXT_ROWS - 1) / PXT_ROWS;
-    const int all = (P + PXT_KEYS - 1) / PXT_KEYS;
-    const int64_t base = (int64_t)o->tc_tiles * nkv;
-    const double per_part = (double)rows * nkv * d * 8 / 8e12 / 0.7e-6;
-    double best = 1e30;
-    for (int s = 1; s <= all && s <= 64; ++s) {
-      const double cost = (double)((base * s + kSms - 1) / kSms) * ((all + s - 1) / s + 4) + s * per_part;
-      if (cost < best) best = cost, o->tc_splits = s;
-    }
-  }
+  o->tc_tiles = rows >= PXT_MIN_ROWS && P > 0 ? (rows + PXT_ROWS - 1) / PXT_ROWS : 0;
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t r = at;
     at += (n + 255) / 256 * 256;
     return r;
   };
-  o->plan_off = take((size_t)(2 * (B + 1) + 2) * 4);
+  o->plan_off = take((size_t)(2 * (B + 1) + 4) * 4);
   o->item_ml = take((size_t)nkv * o->max_tiles * 128);
   o->item_o = take((size_t)nkv * o->max_tiles * 16 * d * 4);
-  o->warp_ml = take((size_t)o->n_warps * 128);
-  o->warp_o = take((size_t)o->n_warps * 16 * d * 4);
-  const size_t slots = (size_t)nkv * o->tc_tiles * o->tc_splits * PXT_ROWS;
-  o->tc_ml = take(slots * 8);
-  o->tc_o = take(slots * d * 4);
+  o->warp_ml = take((size_t)PX_SMS * PXR_WARPS * 128);
+  o->warp_o = take((size_t)PX_SMS * PXR_WARPS * 16 * d * 4);
+  const size_t items = (size_t)nkv * o->tc_tiles * PXT_ROWS, work = o->tc_tiles ? (size_t)PX_SMS * PXT_ROWS : 0;
+  o->tc_item_ml = take(items * 8), o->tc_item_o = take(items * d * 4);
+  o->tc_work_ml = take(work * 8), o->tc_work_o = take(work * d * 4);
   o->total = at;
   return true;
 }
@@ -161,23 +152,26 @@ bool cache_map(CUtensorMap* map, const PagedKv& kv, const void* ptr, int dtype, 
 
 template <typename T, int D>
 int px_launch(PrefixParams& p, const PxPlan& t, int dtype, void* stream) {
-  static std::atomic<unsigned long long> allowed, allowed_tc;
-  if (!allow_smem((const void*)prefix_rows_kernel<T, D>, px_rows_smem(D, PXR_MAX_SEQS + 1), allowed)) return LOOPSPEC_ECUDA;
-  // The prefix on tcgen05: boxes of at least 8 slots (a swizzled group of rows), strides a tensor map takes; else the rows' kernel has it too.
+  static std::atomic<unsigned long long> allowed;
+  if (!allow_smem((const void*)prefix_kernel<T, D>, PxCfg<D>::smem(PX_MAX_SEQS + 1), allowed, 168)) return LOOPSPEC_ECUDA;
+  // The prefix on tcgen05: pages of at least 8 slots (a swizzled group of rows) and strides that a tensor map takes; else it is one more problem of few rows.
   CUtensorMap mk, mv;
+  memset(&mk, 0, sizeof mk), memset(&mv, 0, sizeof mv);
   const int page = 1 << p.kv.page_shift, box = std::min(page, PXT_KEYS);
-  const bool tc = t.tc_splits && page >= 8 && cache_map(&mk, p.kv, p.kv.k, dtype, box) && cache_map(&mv, p.kv, p.kv.v, dtype, box);
-  p.prefix_rows = p.prefix_len > 0 && !tc;
-  if (tc) {
-    p.tc_tiles = t.tc_tiles, p.tc_splits = t.tc_splits;
-    if (!allow_smem((const void*)prefix_tc_kernel<T, D>, pxt_smem(D), allowed_tc)) return LOOPSPEC_ECUDA;
-    prefix_tc_kernel<T, D><<<t.tc_tiles * t.tc_splits * p.kv.n_kv, PXT_THREADS, pxt_smem(D), static_cast<cudaStream_t>(stream)>>>(mk, mv, p);
-    if (cudaGetLastError() != cudaSuccess) return LOOPSPEC_ECUDA;
+  const bool tc = t.tc_tiles && page >= 8 && cache_map(&mk, p.kv, p.kv.k, dtype, box) && cache_map(&mv, p.kv, p.kv.v, dtype, box);
+  p.tc_tiles = tc ? t.tc_tiles : 0, p.prefix_rows = p.prefix_len > 0 && !tc;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3(PX_SMS), cfg.blockDim = dim3(PX_THREADS), cfg.dynamicSmemBytes = PxCfg<D>::smem(p.B + p.prefix_rows), cfg.stream = static_cast<cudaStream_t>(stream);
+  if (cudaLaunchKernelEx(&cfg, prefix_kernel<T, D>, mk, mv, static_cast<const PrefixParams&>(p)) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return LOOPSPEC_ECUDA;
   }
-  const int rc = launch(prefix_rows_kernel<T, D>, dim3(kSms * 2), PXR_WARPS * 32, px_rows_smem(D, p.B + p.prefix_rows), stream, p, tc);
-  if (rc) return rc;
-  const int z = std::max(1, std::min(16, (int)(((int64_t)p.T * p.G / p.B + 3) / 4)));
-  return launch(prefix_merge_kernel<T, D>, dim3(p.kv.n_kv, p.B, z), 128, 0, stream, p, true);
+  // the fold: a CTA per row and query head while there are few, else a warp
+  const int64_t per_seq = ((int64_t)p.T * p.G + p.B - 1) / p.B;
+  if ((int64_t)p.T * p.nq <= 4 * kSms)
+    return launch(prefix_merge_kernel<T, D, 4>, dim3(p.kv.n_kv, p.B, (unsigned)std::min<int64_t>(per_seq, 64)), 128, 0, stream, p, true);
+  return launch(prefix_merge_kernel<T, D, 1>, dim3(p.kv.n_kv, p.B, (unsigned)std::min<int64_t>((per_seq + 3) / 4, 64)), 128, 0, stream, p, true);
 }
 
 // ---- sampling ----
@@ -253,12 +247,13 @@ int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t
   p.page_table = page_table, p.table_ld = table_ld, p.table_w = table_width, p.lens = lens, p.cu_rows = cu_rows;
   p.B = n_seqs, p.T = T, p.nq = n_q_heads;
   p.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)p.kv.d) : scale) * 1.4426950408889634f;
-  p.max_tiles = t.max_tiles, p.n_warps = t.n_warps;
+  p.max_tiles = t.max_tiles;
   unsigned char* sc = static_cast<unsigned char*>(scratch);
   p.plan = reinterpret_cast<int*>(sc + t.plan_off);
   p.item_ml = reinterpret_cast<float*>(sc + t.item_ml), p.item_o = reinterpret_cast<float*>(sc + t.item_o);
   p.warp_ml = reinterpret_cast<float*>(sc + t.warp_ml), p.warp_o = reinterpret_cast<float*>(sc + t.warp_o);
-  p.tc_ml = reinterpret_cast<float*>(sc + t.tc_ml), p.tc_o = reinterpret_cast<float*>(sc + t.tc_o);
+  p.tc_item_ml = reinterpret_cast<float*>(sc + t.tc_item_ml), p.tc_item_o = reinterpret_cast<float*>(sc + t.tc_item_o);
+  p.tc_work_ml = reinterpret_cast<float*>(sc + t.tc_work_ml), p.tc_work_o = reinterpret_cast<float*>(sc + t.tc_work_o);
   p.out = out, p.out_ld = out_ld, p.lse = lse, p.flag = flag;
   if (p.kv.d == 128) return kv->dtype == 1 ? px_launch<__nv_bfloat16, 128>(p, t, 1, cuda_stream) : px_launch<__half, 128>(p, t, 2, cuda_stream);
   return kv->dtype == 1 ? px_launch<__nv_bfloat16, 64>(p, t, 1, cuda_stream) : px_launch<__half, 64>(p, t, 2, cuda_stream);

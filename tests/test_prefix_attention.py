@@ -143,6 +143,33 @@ def test_a_prefix_with_not_a_number_in_one_head():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B", [1, 60])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_a_key_that_is_no_number_shows_in_every_row(B, bad):
+    """Each key of the prefix in turn (by its place in a tile), and an own one: scores that are no number leave none."""
+    for at in list(range(0, 140, 9)) + [299]:
+        s = make(300, [1] * B, [3] * B, 4, 2, 128, 16, "bf16", seed=4)
+        s["kv"][int(s["prefix"][at // 16]), 0, 0, at % 16, 5:7] = bad  # (two elements: inf - inf or a sum of either sign)
+        got, lse = call(s)
+        q = s["q"][:, :2, 5:7].float()
+        score = (q * bad).sum(-1)
+        gone = ~(score == -math.inf)  # (-inf: a weight of nothing)
+        assert got[:, :2][gone].isnan().all() and got[:, :2][~gone].isfinite().all() and got[:, 2:].isfinite().all()
+        assert lse[:, 2:].isfinite().all() and not lse[:, :2][gone].isfinite().any()
+
+
+@pytest.mark.gpu
+def test_references_that_move_often():
+    """Keys whose scores grow along the prefix, so that rows leave their reference behind again and again, and rows that never do."""
+    for d, dt in ((64, "fp16"), (128, "bf16")):
+        s = make(1300, [1] * 80, [40] * 80, 2, 1, d, 16, dt, seed=9, scale=1.0)
+        for j in range(-(-1300 // 16)):
+            s["kv"][int(s["prefix"][j]), 0] *= 1 + j / 8
+        s["q"][::3] *= 0.01
+        check(s, *call(s))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("B", [2, 70])
 def test_scales_strides_streams_and_graphs(B):
     """Large scores (one key takes nearly all), a scale, rows inside wider ones, [page][slot][head] order, a stream of its own, a captured call
