@@ -39,7 +39,7 @@ struct PxCfg {
   static constexpr int TC_TILE = PXT_KEYS * D * 2;
   static constexpr int ROWS_BYTES = PXR_WARPS * STAGES * 2 * TILE, TILES_BYTES = (1 + PXT_K_STAGES + PXT_V_STAGES) * TC_TILE;
   static constexpr int MAIN = 1024 + (ROWS_BYTES > TILES_BYTES ? ROWS_BYTES : TILES_BYTES);
-  static constexpr int smem(int np) { return MAIN + (2 * np + 2) * 4; }
+  static constexpr int smem(int np) { return MAIN + (np + 1) * 4; }
 };
 
 struct PrefixParams {
@@ -57,10 +57,12 @@ struct PrefixParams {
   int B, T, nq, G;
   float scale_log2;        // scale * log2(e)
   int max_tiles;           // row tiles (of 16 rows) a kv head can have
-  int* plan;               // [2 NP + 2]: units before problem i, row tiles before it (the last entries: their totals); then workers of the tiles, CTAs of the rows
-  float *item_o, *item_ml; // rows, partials of the segments that begin with a problem's first key: [kv head][row tile][16][D], ..[2]
-  float *warp_o, *warp_ml; // ... of the others: [warp][16][D], ..[2]
-  float *tc_item_o, *tc_item_ml, *tc_work_o, *tc_work_ml;  // tiles: [kv head][row tile][128][D], ..[2]; [worker][row tile][128][D], ..[2]
+  // partials of the rows' role: of the segments that begin with a problem's first key [kv head][row tile][16][D], ..[2], and of the others [warp][16][D], ..[2]
+  float *item_o, *item_ml, *warp_o, *warp_ml;
+  // ... of the tiles' role: [kv head][row tile][128][D], ..[2]; [worker][row tile][128][D], ..[2]
+  float *tc_item_o, *tc_item_ml, *tc_work_o, *tc_work_ml;
+  int* state;              // 1: the row counts are not what they should be, and nothing of the rows' is done
+  int2 *item_seg, *tc_seg; // for every row tile (of either role): the worker of its first segment and how many workers, one after the other, have segments of it
   void* out;
   long long out_ld;
   float* lse;              // [T][nq] or null
@@ -71,11 +73,11 @@ struct PrefixParams {
 // in the prefix)
 struct PxProblem {
   int row0, n, len;
-  bool prefix, bad;  // bad: row counts that do not ascend in [0, T], a length beyond the table
+  bool prefix, bad_rows, bad_len;  // row counts that do not ascend in [0, T]; a length beyond the table (cut to it)
 };
 __device__ __forceinline__ PxProblem px_problem(const PrefixParams& p, int i) {
   PxProblem r;
-  r.prefix = p.prefix_rows && i == 0, r.bad = false;
+  r.prefix = p.prefix_rows && i == 0, r.bad_rows = r.bad_len = false;
   if (r.prefix) {
     r.row0 = 0, r.n = p.T, r.len = p.prefix_len;
     return r;
@@ -86,23 +88,29 @@ __device__ __forceinline__ PxProblem px_problem(const PrefixParams& p, int i) {
   const bool rows = r0 >= 0 && r1 >= r0 && r1 <= p.T;
   r.row0 = r0, r.n = rows ? r1 - r0 : 0;
   r.len = len < 0 ? 0 : (int)min((long long)len, cap);
-  r.bad = !rows || r.len != len;
+  r.bad_rows = !rows, r.bad_len = r.len != len;
   return r;
 }
 
+// The first of a problem's row tiles: a rule of its own rows, so that nothing has to be added up to find a partial.  (Tiles of 16 rows per sequence are at
+// most its rows / 16 + 1, so that those of two sequences do not meet.)
+__device__ __forceinline__ int px_first_tile(const PrefixParams& p, int i, const PxProblem& r) {
+  return r.prefix ? 0 : (p.prefix_rows ? (p.T * p.G + 15) / 16 : 0) + r.row0 * p.G / 16 + i - p.prefix_rows;
+}
+
 // What precedes x in this CTA plus x, and the total (all threads of the CTA)
-__device__ __forceinline__ long long px_block_scan(long long x, long long* s_w, long long& total) {
+__device__ __forceinline__ int px_block_scan(int x, int* s_w, int& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
   __syncthreads();
   if (lane == 31) s_w[warp] = x;
   __syncthreads();
   total = 0;
-  long long add = 0;
+  int add = 0;
   for (int w = 0; w < PX_THREADS / 32; ++w) {
     if (w == warp) add = total;
     total += s_w[w];
@@ -163,7 +171,7 @@ struct PxRoles {
 // first keys, last weights, partial), an SM streams some 50 bytes a ns.  Of all numbers of workers that leave the rows a CTA, the one with which the later of
 // the two roles ends first, a thread for each; as many as a multiple of the heads, or a part of them, have no segment cut at the end of one.
 template <int D>
-__device__ __forceinline__ PxRoles px_roles(const PrefixParams& p, long long row_units, long long* s_w) {
+__device__ __forceinline__ PxRoles px_roles(const PrefixParams& p, long long row_units, unsigned long long* s_w) {
   PxRoles r = {0, 0};
   if (p.tc_tiles == 0) return r;
   const int all = (p.prefix_len + PXT_KEYS - 1) / PXT_KEYS, most = PX_SMS - (row_units > 0), w = threadIdx.x + 1, lane = threadIdx.x & 31;
@@ -186,9 +194,9 @@ __device__ __forceinline__ PxRoles px_roles(const PrefixParams& p, long long row
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
   __syncthreads();
-  if (lane == 0) s_w[threadIdx.x >> 5] = (long long)best;
+  if (lane == 0) s_w[threadIdx.x >> 5] = best;
   __syncthreads();
-  for (int i = 0; i < PX_THREADS / 32; ++i) best = min(best, (unsigned long long)s_w[i]);
+  for (int i = 0; i < PX_THREADS / 32; ++i) best = min(best, s_w[i]);
   r.workers = (int)(unsigned)best, r.tiles = tiles_of(r.workers, rounds);
   return r;
 }
@@ -203,7 +211,7 @@ __device__ __forceinline__ PxRoles px_roles(const PrefixParams& p, long long row
 // role a row's reference moves only when a tile's maximum runs more than 2^8 ahead of it, so that a tile mostly needs neither a maximum over its lanes
 // nor a rescaled accumulator.
 template <typename T, int D>
-__device__ __forceinline__ void px_rows_role(const PrefixParams& p, unsigned char* raw, const int* s_unit, const int* s_item, int Us, int cta, int n_cta) {
+__device__ __forceinline__ void px_rows_role(const PrefixParams& p, unsigned char* raw, const int* s_unit, int Us, int cta, int n_cta) {
   constexpr int TILE = PxCfg<D>::TILE, STAGES = PxCfg<D>::STAGES, KS = D / 16, NT = D / 8, NH = D / 64, PIECE = PXR_KEYS * 128;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), g = lane >> 2, t = lane & 3;
   const int NP = p.B + p.prefix_rows;
@@ -436,7 +444,8 @@ __device__ __forceinline__ void px_rows_role(const PrefixParams& p, unsigned cha
 
     // ---- the segment is done ----
     const bool whole = first_k == 0;
-    const long long slot = whole ? (long long)cc.h * p.max_tiles + s_item[cc.i] + cc.rt : w;
+    const long long slot = whole ? (long long)cc.h * p.max_tiles + px_first_tile(p, cc.i, cc.r) + cc.rt : w;
+    if (whole && lane == 0) p.item_seg[slot] = make_int2(w, seg == cc.n_k ? 1 : 1 + px_worker_of(u + cc.n_k - 1, U, W) - w);
     float* po = (whole ? p.item_o : p.warp_o) + slot * 16 * D;
     float* pm = (whole ? p.item_ml : p.warp_ml) + slot * 32;
 #pragma unroll

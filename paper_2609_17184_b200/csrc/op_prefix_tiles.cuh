@@ -112,7 +112,7 @@ struct PxtShared {
 // more than the CTAs, row tiles cta, cta + n_cta, .. of the one worker.
 struct PxtWork {
   long long u_lo, u_hi;
-  int worker, rt0, rt_step, all, last_keys, R;
+  int worker, workers, rt0, rt_step, all, last_keys, R;
   unsigned base, k_ring, v_ring;  // shared addresses: queries, rings
   unsigned char* base_ptr;
   template <int D>
@@ -120,7 +120,7 @@ struct PxtWork {
     PxtWork w;
     const bool one = p.tc_tiles > roles.tiles;
     w.all = (p.prefix_len + PXT_KEYS - 1) / PXT_KEYS, w.last_keys = p.prefix_len - (w.all - 1) * PXT_KEYS, w.R = p.T * p.G;
-    w.worker = one ? 0 : cta / p.tc_tiles, w.rt0 = one ? cta : cta % p.tc_tiles, w.rt_step = one ? roles.tiles : p.tc_tiles;
+    w.workers = roles.workers, w.worker = one ? 0 : cta / p.tc_tiles, w.rt0 = one ? cta : cta % p.tc_tiles, w.rt_step = one ? roles.tiles : p.tc_tiles;
     const long long U = (long long)p.kv.n_kv * w.all;
     w.u_lo = w.worker * U / roles.workers, w.u_hi = (w.worker + 1) * U / roles.workers;
     w.base = (tc_smem_u32(raw) + 1023u) & ~1023u, w.k_ring = w.base + PxCfg<D>::TC_TILE, w.v_ring = w.k_ring + PXT_K_STAGES * PxCfg<D>::TC_TILE;
@@ -388,6 +388,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
     float* pm = (k_lo == 0 ? p.tc_item_ml : p.tc_work_ml) + (tile * PXT_ROWS + row) * 2;
     const bool live = r0 + row < w.R;
     if (live && st == 0) __stcg(reinterpret_cast<float2*>(pm), make_float2(top, mass));
+    if (k_lo == 0 && tid == 0) p.tc_seg[tile] = make_int2(w.worker, n == w.all ? 1 : 1 + px_worker_of((long long)(h + 1) * w.all - 1, (long long)p.kv.n_kv * w.all, w.workers) - w.worker);
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
       unsigned o[32];

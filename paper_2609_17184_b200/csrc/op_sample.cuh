@@ -28,6 +28,7 @@ constexpr int NV = 7;              // sums taken together
 constexpr int BINS = 2 * THREADS;  // of the distance from the best logit, as far down as a token weighs anything
 constexpr int LIST = 2048;         // tokens one CTA can be sent, an equal part of them by each CTA
 constexpr int SOLO = 256;          // candidates with which one CTA finishes a row alone
+static_assert(2 * SOLO == THREADS, "the list's companion holds a pair for each of them, or a sum for each thread");
 constexpr int MAX_VOCAB_BITS = 18;
 
 struct Params {
@@ -85,6 +86,10 @@ struct Weigher {
     double y = (widen(z) - top) * c;
     // (y <= 0: a larger high word is further down; the low word does not matter there)
     y = __hiloint2double((int)min(z > none ? (unsigned)__double2hiint(y) : 0xffffffffu, far), __double2loint(y));
+    return power(y);
+  }
+  // 2^(S + y / 256) for a y from 0 down to -256 (S + 2)
+  __device__ __forceinline__ double power(double y) const {
     const double magic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low word is y to the nearest integer
     const double t = y + magic;
     const int k = __double2loint(t);
@@ -155,8 +160,29 @@ struct Cluster {
       v[i] = r;
     }
   }
-  // What precedes this thread's x in this CTA, and its total
-  __device__ __forceinline__ u64 scan_block(u64 x, u64& total) {
+  // What precedes this thread's x in this CTA, and its total; and the same of a second value
+  __device__ __forceinline__ u64 scan_block(u64 x, u64& total, u64 x2, u64& before2, u64& total2) const {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    u64 inc = x, inc2 = x2;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 t = __shfl_up_sync(0xffffffffu, inc, o), t2 = __shfl_up_sync(0xffffffffu, inc2, o);
+      if (lane >= o) inc += t, inc2 += t2;
+    }
+    __syncthreads();
+    if (lane == 31) sh[warp] = inc, sh[WARPS + warp] = inc2;
+    __syncthreads();
+    u64 before = inc - x;
+    before2 = inc2 - x2, total = total2 = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const u64 s = sh[w], s2 = sh[WARPS + w];
+      if (w < warp) before += s, before2 += s2;
+      total += s, total2 += s2;
+    }
+    return before;
+  }
+  __device__ __forceinline__ u64 scan_block(u64 x, u64& total) const {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     u64 inc = x;
 #pragma unroll
@@ -178,7 +204,7 @@ struct Cluster {
     return before;
   }
   // a[0 .. n) ascending (a has room for the next power of two)
-  __device__ __forceinline__ void sort(u64* a, int n) {
+  __device__ __noinline__ void sort(u64* a, int n) const {
     int size = 2;
     while (size < n) size *= 2;
     for (int i = n + threadIdx.x; i < size; i += THREADS) a[i] = ~0ull;
@@ -210,6 +236,21 @@ struct Cluster {
   }
 };
 
+// four neighbouring logits of a slice
+template <typename T>
+__device__ __forceinline__ float4 quad_of(const void* z_sm, int i) {
+  if constexpr (sizeof(T) == 4) {
+    return reinterpret_cast<const float4*>(z_sm)[i];
+  } else {
+    const uint2 w = reinterpret_cast<const uint2*>(z_sm)[i];
+    const T* e = reinterpret_cast<const T*>(&w);
+    return make_float4(to_f32<T>(e[0]), to_f32<T>(e[1]), to_f32<T>(e[2]), to_f32<T>(e[3]));
+  }
+}
+// One logit's weight where few are taken.  (Out of line: a row runs this code once, and what is not in the instruction cache costs its way from the
+// L2 - inlined throughout, the kernel was 390 KB.)
+__device__ __noinline__ double weigh_one(const Weigher& g, float z) { return g.scaled(z); }
+
 template <typename T>
 __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constant__ Params p) {
   extern __shared__ __align__(16) unsigned char smp_smem[];
@@ -225,48 +266,31 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   const float top_p = p.top_p ? __ldg(p.top_p + row) : 1.f, min_p = p.min_p ? __ldg(p.min_p + row) : 0.f;
   const int top_k = p.top_k ? __ldg(p.top_k + row) : 0;
 
-  // ---- the slice, in pieces of 16 bytes as they lie in memory; an element that is no number counts as masked out ----
+  // ---- the slice as it lies in memory, 16 bytes at a time; what of the first and the last 16 is not the slice's counts as masked out.  (A logit that is
+  // no number is treated so wherever it is compared.) ----
   constexpr int VEC = 16 / sizeof(T);
   const T* src = static_cast<const T*>(p.logits) + row * p.ld + v_lo;
   const int head = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));  // elements from the 16-byte boundary before the slice
-  const int n_piece = (head + n + VEC - 1) / VEC;
-  uint4* z_sm = reinterpret_cast<uint4*>(smp_smem);  // piece i: tokens v_lo - head + VEC i ..; masked out where they are not this slice's
-  auto unpack = [](const uint4& w, float (&z)[VEC]) {
-    const T* e = reinterpret_cast<const T*>(&w);
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) z[j] = to_f32<T>(e[j]);
-  };
+  const int n_piece = (head + n + VEC - 1) / VEC, whole = (head + n) / VEC, n_quad = n_piece * (VEC / 4), v_first = v_lo - head;
+  unsigned char* z_sm = smp_smem;  // element e: token v_first + e
   float top = -INFINITY;
   {
     const uint4* vs = reinterpret_cast<const uint4*>(src - head);
 #pragma unroll 4
-    for (int i = tid; i < n_piece; i += THREADS) {
-      const int e0 = i * VEC - head;
-      uint4 w;
-      T* e = reinterpret_cast<T*>(&w);
-      if (e0 >= 0 && e0 + VEC <= n) w = __ldcs(vs + i);
-      else
+    for (int i = tid + (head != 0); i < whole; i += THREADS) {
+      const uint4 w = __ldcs(vs + i);
+      reinterpret_cast<uint4*>(z_sm)[i] = w;
+      const T* e = reinterpret_cast<const T*>(&w);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) e[j] = e0 + j >= 0 && e0 + j < n ? src[e0 + j] : T(-INFINITY);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float z = to_f32<T>(e[j]);
-        if (z != z) e[j] = T(-INFINITY);
-        top = fmaxf(top, z);  // (of a number and none: the number)
-      }
-      z_sm[i] = w;
+      for (int j = 0; j < VEC; ++j) top = fmaxf(top, to_f32<T>(e[j]));  // (of a number and none: the number)
+    }
+    const int e = tid < VEC ? tid : whole * VEC + tid - VEC;  // the first piece's and the last one's elements
+    if (tid < VEC ? head != 0 || whole == 0 : tid < 2 * VEC && whole < n_piece && (whole > 0 || head == 0)) {
+      const T z = e >= head && e < head + n ? src[e - head] : T(-INFINITY);
+      reinterpret_cast<T*>(z_sm)[e] = z, top = fmaxf(top, to_f32<T>(z));
     }
   }
   if (tid < 256) s_table[tid] = exp2((double)tid / 256);
-  // f(logits of a piece, token of its first) for this thread's pieces
-  auto each = [&](auto f) {
-#pragma unroll 2
-    for (int i = tid; i < n_piece; i += THREADS) {
-      float z[VEC];
-      unpack(z_sm[i], z);
-      f(z, v_lo - head + i * VEC);
-    }
-  };
   const unsigned top_key = (unsigned)R.max(key_of(top));
   top = logit_of(top_key);
   auto put = [&](int token, float prob) {
@@ -280,11 +304,12 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   }
   if (!(temp > 0.f)) {  // greedy: the first of the largest
     unsigned first = 0;
-    each([&](const float (&z)[VEC], int v) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j)
-        if (z[j] == top) first = max(first, 0x7fffffffu - (unsigned)(v + j));
-    });
+#pragma unroll 1
+    for (int i = tid; i < n_quad; i += THREADS) {
+      const float4 q = quad_of<T>(z_sm, i);
+      const int j = q.x == top ? 0 : q.y == top ? 1 : q.z == top ? 2 : q.w == top ? 3 : 4;
+      if (j < 4) first = max(first, 0x7fffffffu - (unsigned)(v_first + i * 4 + j));
+    }
     first = (unsigned)R.max(first);
     if (writer) put((int)(0x7fffffffu - first), 1.f);
     return;
@@ -303,6 +328,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     // of top-p comes out to within a bin or two.  Tokens too far down to weigh anything are in no bin: a cut among them cuts nothing.
     unsigned* hist = reinterpret_cast<unsigned*>(smp_smem + p.hist_off);  // [BINS]: tokens, then [BINS]: how far down
     u64* list = reinterpret_cast<u64*>(hist + 2 * BINS);
+    u64* weights = list + LIST;
     const float scale = (float)fmin(BINS / (double)(p.shift + 2) * log2_t, 1e30);  // (rounded alike for all: the bins are as monotonous as the logits)
     const double step = log2_t > 0.0 ? log2_t / (double)scale : 0.0;               // log2 of the weights' ratio from one end of a bin to the other
     auto depth_of = [&](float z) -> float {  // BINS or more: in no bin
@@ -312,9 +338,12 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     for (int i = tid; i < BINS / 2; i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
     if (tid == 0) s_cut = ~0ull, s_mine[0] = s_mine[1] = 0, s_found[0] = s_found[1] = s_found[2] = BINS;
     __syncthreads();
-    each([&](const float (&z)[VEC], int) {
+#pragma unroll 2
+    for (int i = tid; i < n_quad; i += THREADS) {
+      const float4 q = quad_of<T>(z_sm, i);
+      const float z[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
+      for (int j = 0; j < 4; ++j) {
         const float d = depth_of(z[j]);
         if (d < (float)BINS) {
           const int b = (int)d;
@@ -322,23 +351,15 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
           if (by_p) atomicAdd(hist + BINS + b, (unsigned)((d - (float)b) * 1024.f));
         }
       }
-    });
+    }
     cl.sync();
     // this thread's two bins in the whole cluster
     u64 cnt[2] = {0, 0}, low[2] = {0, 0};
-    {
-      uint2 c[MAX_CS], l[MAX_CS];
-#pragma unroll
-      for (int q = 0; q < MAX_CS; ++q) {
-        const unsigned* h = cl.map_shared_rank(hist, min(q, R.n - 1)) + 2 * tid;
-        c[q] = l[q] = make_uint2(0, 0);
-        if (q < R.n) {
-          c[q] = *reinterpret_cast<const uint2*>(h);
-          if (by_p) l[q] = *reinterpret_cast<const uint2*>(h + BINS);
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < MAX_CS; ++q) cnt[0] += c[q].x, cnt[1] += c[q].y, low[0] += l[q].x, low[1] += l[q].y;
+#pragma unroll 8
+    for (int q = 0; q < R.n; ++q) {
+      const unsigned* h = cl.map_shared_rank(hist, q) + 2 * tid;
+      const uint2 c = *reinterpret_cast<const uint2*>(h), l = *reinterpret_cast<const uint2*>(h + BINS);
+      cnt[0] += c.x, cnt[1] += c.y, low[0] += l.x, low[1] += l.y;
     }
     // the first bin at whose end the sum of w over the bins reaches target: s_found[slot]; the sum before it: s_before[slot]
     auto crossing = [&](u64 before, u64 w0, u64 w1, u64 target, int slot) {
@@ -357,265 +378,276 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
       b_k = s_found[0];
       if (b_k < BINS) of_b_k = top_k - s_before[0];
     }
-    // Bins between which top-p cuts.  Weights of a bin of c tokens and summed depths D (in bins; c / 1024 may be missing): with r = 2^-step, at
-    // depth x of it r^x <= 1 - x (1 - r) (chord) and r^x >= 1 + x ln r (tangent), times the weight at the bin's upper end.
-    int b_lo = 0, b_hi = BINS - 1;
-    auto bracket = [&]() {
-      u64 up[2], down[2];
-      const double r = exp2(-step);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int b = 2 * tid + j;
-        const bool part = b == b_k;  // of the bin where top-k cut only of_b_k tokens are left, whichever
-        const double c = b < b_k ? (double)cnt[j] : part ? (double)of_b_k : 0.0, at = exp2(-b * step) * one;
-        const double d0 = part ? 0.0 : (double)low[j] / 1024, d1 = part ? c : fmin(c, ((double)low[j] + c) / 1024);
-        up[j] = (u64)(at * (c - d0 * (1.0 - r)) * (1.0 + 1e-5) + c);
-        down[j] = (u64)(at * fmax(c + d1 * -0.69314718055994530942 * step, c * r) * (1.0 - 1e-5));  // (1e-5: the roundings of a depth)
-        if (down[j] > (u64)c) down[j] -= (u64)c;  // (weights are rounded)
-        else down[j] = 0;
-      }
-      u64 up_all, down_all;
-      const u64 up_before = R.scan_block(up[0] + up[1], up_all), down_before = R.scan_block(down[0] + down[1], down_all);
-      crossing(up_before, up[0], up[1], times<true>(top_p, down_all), 1);    // the mass may be this small: it is reached here at the earliest
-      crossing(down_before, down[0], down[1], times<true>(top_p, up_all), 2);  // ... or this large
-      __syncthreads();
-      b_lo = min(s_found[1], BINS - 1), b_hi = min(s_found[2], min(b_k, BINS - 1));
-    };
-    if (by_p && !by_k) bracket();
-    auto count_to = [&](int b) -> u64 {  // tokens of the bins up to b
-      if (2 * tid == (b & ~1)) s_upto = n_before + cnt[0] + (b & 1 ? cnt[1] : 0);
-      __syncthreads();
-      return s_upto;
-    };
-    // Sends this CTA's tokens of the bins b0 .. b1, in no order, to its part of CTA 0's list, and their number to all; with MASS, also: the exact weight
-    // of what is kept so far, and the part of it in the bins before b0.  Complete after the next barrier of the cluster.
-    u64 sums[2] = {0, 0};
     const unsigned room = LIST / R.n;
-    auto send = [&](int which, int b0, int b1, auto mass) {
-      u64* to = cl.map_shared_rank(list, 0) + R.rank * room;
-      const float f0 = (float)b0, f1 = (float)(b1 + 1);  // (b1 < BINS)
-      each([&](const float (&z)[VEC], int v) {
+    bool solo = false;
+    u64 all = 0;  // the mass top-p is a part of
+    // First top-k (or, where few tokens are candidates at all, whatever cuts there are), then top-p
+#pragma unroll 1
+    for (int step_ = 0; step_ < 2; ++step_) {
+      int b_lo = 0, b_hi = BINS - 1;
+      if (by_p && by_k == (step_ == 1)) {
+        // Bins between which top-p cuts.  Weights of a bin of c tokens and summed depths D (in bins; c / 1024 may be missing): with r = 2^-step, at
+        // depth x of it r^x <= 1 - x (1 - r) (chord) and r^x >= 1 + x ln r (tangent), times the weight at the bin's upper end.
+        u64 up[2], down[2];
+        const double limit = -256.0 * (p.shift + 2), r = weigh.power(fmax(-256.0 * step, limit)) / one;
+#pragma unroll 1
+        for (int j = 0; j < 2; ++j) {
+          const int b = 2 * tid + j;
+          const bool part = b == b_k;  // of the bin where top-k cut only of_b_k tokens are left, whichever
+          const double c = b < b_k ? (double)(j ? cnt[1] : cnt[0]) : part ? (double)of_b_k : 0.0, deep = (double)(j ? low[1] : low[0]) / 1024;
+          const double at = weigh.power(fmax(-256.0 * step * b, limit));
+          const double d0 = part ? 0.0 : deep, d1 = part ? c : fmin(c, deep + c / 1024);
+          const u64 hi = (u64)(at * (c - d0 * (1.0 - r)) * (1.0 + 1e-5) + c);
+          u64 lo = (u64)(at * fmax(c + d1 * -0.69314718055994530942 * step, c * r) * (1.0 - 1e-5));  // (1e-5: the roundings of a depth)
+          lo = lo > (u64)c ? lo - (u64)c : 0;                                                        // (weights are rounded)
+          if (j) up[1] = hi, down[1] = lo;
+          else up[0] = hi, down[0] = lo;
+        }
+        u64 up_all, down_all, down_before;
+        const u64 up_before = R.scan_block(up[0] + up[1], up_all, down[0] + down[1], down_before, down_all);
+        crossing(up_before, up[0], up[1], times<true>(top_p, down_all), 1);      // the mass may be this small: it is reached here at the earliest
+        crossing(down_before, down[0], down[1], times<true>(top_p, up_all), 2);  // ... or this large
+        __syncthreads();
+        b_lo = min(s_found[1], BINS - 1), b_hi = min(s_found[2], min(b_k, BINS - 1));
+      }
+      if (step_ == 0) {
+        const int b_end = by_k ? min(b_k, BINS - 1) : b_hi;
+        if (2 * tid == (b_end & ~1)) s_upto = n_before + cnt[0] + (b_end & 1 ? cnt[1] : 0);
+        __syncthreads();
+        solo = s_upto <= SOLO;
+        if (solo) b_lo = 0, b_hi = b_end;
+        else if (b_k < BINS) b_lo = b_hi = b_k;
+        else if (!by_p || by_k) continue;  // (no cut, or top-p's is to come)
+      } else if (!by_p || !by_k) {
+        break;  // (found in the first turn)
+      }
+      const bool k_cut = by_k && step_ == 0, mass = by_p && !k_cut;
+      // ---- this CTA's tokens of the bins b_lo .. b_hi go, in no order, to its part of CTA 0's list, and their number to all; with `mass`, also: the exact weight
+      // of what is kept so far, and the part of it in the bins before b_lo ----
+      u64 sums[2] = {0, 0};
+      {
+        u64* to = cl.map_shared_rank(list, 0) + R.rank * room;
+        const float f0 = (float)b_lo, f1 = (float)(b_hi + 1);  // (b_hi < BINS)
+#pragma unroll 2
+        for (int i = tid; i < n_quad; i += THREADS) {
+          const float4 q = quad_of<T>(z_sm, i);
+          const float z[4] = {q.x, q.y, q.z, q.w};
+          if (mass) {
+            u64 w[4];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const float d = depth_of(z[j]);
-          if constexpr (mass.value) {
-            u64 w = weigh(z[j]);
-            if (cut != ~0ull && place_of(z[j], v + j) > cut) w = 0;
-            sums[0] += w, sums[1] += d < f0 ? w : 0;
+            for (int j = 0; j < 4; ++j) w[j] = weigh(z[j]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (cut != ~0ull && place_of(z[j], v_first + i * 4 + j) > cut) w[j] = 0;
+              sums[0] += w[j], sums[1] += depth_of(z[j]) < f0 ? w[j] : 0;
+            }
           }
-          if (d >= f0 && d < f1) {
-            const unsigned at = atomicAdd(s_mine + which, 1u);
-            if (at < room) to[at] = place_of(z[j], v + j);
-          }
-        }
-      });
-      __syncthreads();
-      if (tid < R.n) *cl.map_shared_rank(&s_sent[which][R.rank], tid) = s_mine[which];
-    };
-    // CTA 0 closes the gaps in its list (all its threads call); the tokens in it
-    auto collect = [&](int which) -> int {
-      u64 e[LIST / THREADS];
-      int at[LIST / THREADS], all = 0;
 #pragma unroll
-      for (int j = 0; j < LIST / THREADS; ++j) {
-        const int i = tid + j * THREADS, q = i / (int)room, k = i - q * (int)room;
-        e[j] = list[i], at[j] = -1;
-        if (q < R.n && k < (int)s_sent[which][q]) {
-          at[j] = k;
-          for (int x = 0; x < q; ++x) at[j] += s_sent[which][x];
-        }
-      }
-      for (int q = 0; q < R.n; ++q) all += s_sent[which][q];
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < LIST / THREADS; ++j)
-        if (at[j] >= 0) list[at[j]] = e[j];
-      __syncthreads();
-      return all;
-    };
-    // Up to SOLO tokens in the list: a group of threads for each goes over all others.  This thread's token, its number in the list (SOLO and more:
-    // none), the number of its group's threads that are ahead of it
-    u64* weights = list + LIST;
-    struct Mine {
-      u64 place;
-      int at, part, lanes;
-    };
-    auto mine_of = [&](int N) -> Mine {
-      int lanes = 32;
-      while (lanes * N > THREADS) lanes >>= 1;
-      const int at = tid / lanes;
-      return {at < N ? list[at] : ~0ull, at, tid & (lanes - 1), lanes};
-    };
-    // sum of the weights, and the number, of the tokens for which the test holds
-    auto over_others = [&](const Mine& m, int N, auto test, u64& sum, int& count) {
-      sum = 0, count = 0;
-      for (int i = m.part; i < N; i += m.lanes)
-        if (test(list[i])) sum += weights[i], ++count;
-      for (int o = m.lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o), count += __shfl_xor_sync(0xffffffffu, count, o);
-    };
-    const int b_end = by_k ? min(b_k, BINS - 1) : b_hi;
-    const u64 n_cand = count_to(b_end);
-    if (n_cand <= SOLO) {
-      // ---- few candidates: CTA 0 does the rest with a group of threads for each, which goes over all others ----
-      if (by_p && !by_k) {
-        send(0, 0, b_end, std::true_type{});
-        R.sum(sums);
-      } else {
-        send(0, 0, b_end, std::false_type{});
-        cl.sync();
-      }
-      if (R.rank != 0) return;
-      const int N = collect(0);
-      const Mine m = mine_of(N);
-      const bool first = m.at < N && m.part == 0;
-      const double wd = m.at < N ? weigh.scaled(logit_at(m.place)) : 0.0;
-      const u64 w = Weigher::rounded(wd);
-      if (first) weights[m.at] = w;
-      __syncthreads();
-      u64 before;
-      int rank;
-      over_others(m, N, [&](u64 x) { return x < m.place; }, before, rank);
-      u64 s[1] = {0};
-      const bool in_k = m.at < N && (!by_k || rank < top_k);
-      u64 target = ~0ull;
-      if (by_p) {
-        if (by_k) {
-          s[0] = first && in_k ? w : 0;
-          R.sum_block(s);
-          target = times<true>(top_p, s[0]);
-        } else {
-          target = times<true>(top_p, sums[0]);
-        }
-      }
-      const bool stays = in_k && before < target && wd >= least;
-      __syncthreads();
-      if (first && !stays) weights[m.at] = 0;
-      s[0] = first && stays ? w : 0;
-      R.sum_block(s);
-      const u64 total = s[0], at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;
-      over_others(m, N, [&](u64 x) { return token_at(x) < token_at(m.place); }, before, rank);
-      if (first && stays && before <= at && at < before + w) put(token_at(m.place), (float)(wd / (double)total));
-      return;
-    }
-
-    // ---- many tokens stay: only those of the bins where a cut lies are sent ----
-    // The smallest place c such that the sum of val(logit, place) over the places up to c reaches target, among all CTAs' tokens of the bins b0 ..
-    // b1: three bits of it a pass.  For lists that do not fit (many equal logits).
-    auto search = [&](int b0, int b1, auto val, u64 target) -> u64 {
-      u64 c = 0, base = 0;
-      for (int shift = 48; shift >= 0; shift -= 3) {
-        u64 s[NV];
-#pragma unroll
-        for (int k = 0; k < NV; ++k) s[k] = 0;
-        each([&](const float (&z)[VEC], int v) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
+          for (int j = 0; j < 4; ++j) {
             const float d = depth_of(z[j]);
-            const u64 place = place_of(z[j], v + j);
-            if (!(d >= (float)b0 && d < (float)(b1 + 1)) || place >> (shift + 3) != c >> (shift + 3)) continue;
-            const u64 x = val(z[j], place);
+            if (d >= f0 && d < f1) {
+              const unsigned at = atomicAdd(s_mine + step_, 1u);
+              if (at < room) to[at] = place_of(z[j], v_first + i * 4 + j);
+            }
+          }
+        }
+        __syncthreads();
+        if (tid < R.n) *cl.map_shared_rank(&s_sent[step_][R.rank], tid) = s_mine[step_];
+      }
+      R.sum(sums);  // (and what was sent has arrived)
+      if (mass) all = sums[0];
+      unsigned most = 0;
+      for (int q = 0; q < R.n; ++q) most = max(most, s_sent[step_][q]);
+      const u64 target = k_cut ? of_b_k : times<true>(top_p, all) - sums[1];
+      if (most <= room) {
+        if (R.rank == 0) {
+          // ---- CTA 0 closes the gaps in its list ----
+          int N = 0;
+          {
+            u64 e[LIST / THREADS];
+            int at[LIST / THREADS];
+#pragma unroll
+            for (int j = 0; j < LIST / THREADS; ++j) {
+              const int i = tid + j * THREADS, q = i / (int)room, k = i - q * (int)room;
+              e[j] = list[i], at[j] = -1;
+              if (q < R.n && k < (int)s_sent[step_][q]) {
+                at[j] = k;
+                for (int x = 0; x < q; ++x) at[j] += s_sent[step_][x];
+              }
+            }
+            for (int q = 0; q < R.n; ++q) N += s_sent[step_][q];
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < LIST / THREADS; ++j)
+              if (at[j] >= 0) list[at[j]] = e[j];
+            __syncthreads();
+          }
+          auto tell = [&](u64 c) {
+            for (int q = 0; q < R.n; ++q) *cl.map_shared_rank(&s_cut, q) = c;
+          };
+          auto worth = [&](u64 place) -> u64 {  // in the sum that is to reach the target
+            return k_cut ? 1 : place <= cut ? Weigher::rounded(weigh_one(weigh, logit_at(place))) : 0;
+          };
+          u64 goal = target;
+          if (N > SOLO) {
+            // the bins are cut finer, a thread each, and only the part where the target is reached stays in the list
+            u64* fine = weights;  // [THREADS]
+            fine[tid] = 0;
+            if (tid == 0) s_mine[0] = 0;
+            __syncthreads();
+            const float f0 = (float)b_lo, per = THREADS / (float)(b_hi + 1 - b_lo);
+            auto part_of = [&](u64 place) -> int { return min((int)((depth_of(logit_at(place)) - f0) * per), THREADS - 1); };
+            u64 e[LIST / THREADS];
+#pragma unroll 1
+            for (int i = tid; i < N; i += THREADS) {
+              const u64 place = list[i];
+              atomicAdd(fine + part_of(place), worth(place));
+            }
+            __syncthreads();
+            u64 total;
+            const u64 mine = fine[tid], before = R.scan_block(mine, total);
+            if (before < goal && goal <= before + mine) s_found[0] = tid, s_before[0] = before;
+            __syncthreads();
+            const int where = s_found[0];
+            goal -= s_before[0];
+#pragma unroll
+            for (int j = 0; j < LIST / THREADS; ++j) e[j] = tid + j * THREADS < N ? list[tid + j * THREADS] : ~0ull;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < LIST / THREADS; ++j)
+              if (e[j] != ~0ull && part_of(e[j]) == where) list[atomicAdd(s_mine, 1u)] = e[j];
+            __syncthreads();
+            N = (int)s_mine[0];
+          }
+          if (N <= SOLO) {
+            // Few tokens: a group of threads for each, which goes over all others.  First what precedes it in the ranking: how many, and their weight
+            ulonglong2* pairs = reinterpret_cast<ulonglong2*>(weights);  // [SOLO]: place, weight
+            int lanes = 32;
+            while (lanes * N > THREADS) lanes >>= 1;
+            const int at_ = tid / lanes, part = tid & (lanes - 1);
+            const bool have = at_ < N, first = have && part == 0;
+            const u64 place = have ? list[at_] : ~0ull;
+            double wd = 0.0;
+            u64 w = 0;
+            if (have) {
+              if (solo) wd = weigh_one(weigh, logit_at(place)), w = Weigher::rounded(wd);
+              else w = worth(place);
+            }
+            if (first) pairs[at_] = make_ulonglong2(place, w);
+            __syncthreads();
+            u64 before = 0;
+            int rank = 0;
+#pragma unroll 4
+            for (int i = part; i < N; i += lanes) {
+              const ulonglong2 x = pairs[i];
+              if (x.x < place) before += x.y, ++rank;
+            }
+            for (int o = lanes >> 1; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o), rank += __shfl_xor_sync(0xffffffffu, rank, o);
+            if (!solo) {
+              if (first && before < goal && goal <= before + w) tell(place);
+            } else {
+              const bool in_k = have && (!by_k || rank < top_k);
+              u64 s[1] = {first && in_k ? w : 0};
+              if (by_k && by_p) R.sum_block(s);
+              const u64 reach = by_p ? times<true>(top_p, by_k ? s[0] : all) : ~0ull;
+              const bool stays = in_k && before < reach && wd >= least;
+              __syncthreads();
+              if (first && !stays) pairs[at_].y = 0;
+              s[0] = first && stays ? w : 0;
+              R.sum_block(s);
+              const u64 total = s[0], at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;
+              // ... and now, of those that stay, what precedes it by index
+              const unsigned token = (unsigned)token_at(place);
+              before = 0;
+#pragma unroll 4
+              for (int i = part; i < N; i += lanes) {
+                const ulonglong2 x = pairs[i];
+                if ((unsigned)token_at(x.x) < token) before += x.y;
+              }
+              for (int o = lanes >> 1; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+              if (first && stays && before <= at && at < before + w) put((int)token, (float)(wd / (double)total));
+              return;
+            }
+          } else {
+            R.sort(list, N);
+            constexpr int PER = LIST / THREADS;
+            u64 w[PER], sum = 0, total;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) w[j] = tid * PER + j < N ? worth(list[tid * PER + j]) : 0, sum += w[j];
+            u64 before = R.scan_block(sum, total);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+              if (before < goal && goal <= before + w[j]) tell(list[tid * PER + j]);
+              before += w[j];
+            }
+          }
+        }
+        if (solo) return;
+        cl.sync();
+        cut = min(cut, s_cut);
+      } else {
+        // ---- more than fit (many equal logits): the smallest place c such that the sum over the places up to c reaches target, three bits of it a pass of all CTAs ----
+        u64 c = 0, base = 0;
+#pragma unroll 1
+        for (int shift = 48; shift >= 0; shift -= 3) {
+          u64 s[NV];
+#pragma unroll
+          for (int k = 0; k < NV; ++k) s[k] = 0;
+#pragma unroll 1
+          for (int e = tid; e < n_quad * 4; e += THREADS) {
+            const float z = to_f32<T>(reinterpret_cast<const T*>(z_sm)[e]), d = depth_of(z);
+            const u64 place = place_of(z, v_first + e);
+            if (!(d >= (float)b_lo && d < (float)(b_hi + 1)) || place >> (shift + 3) != c >> (shift + 3)) continue;
+            const u64 x = k_cut ? 1 : place <= cut ? Weigher::rounded(weigh_one(weigh, z)) : 0;
             const int digit = (int)(place >> shift) & 7;
 #pragma unroll
             for (int k = 0; k < NV; ++k) s[k] += digit <= k ? x : 0;
           }
-        });
-        R.sum(s);
-        int digit = NV;
+          R.sum(s);
+          int digit = NV;
+          u64 skipped = 0;
 #pragma unroll
-        for (int k = NV - 1; k >= 0; --k)
-          if (base + s[k] >= target) digit = k;
-        u64 skipped = 0;
+          for (int k = NV - 1; k >= 0; --k)
+            if (base + s[k] >= target) digit = k;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-          if (k + 1 == digit) skipped = s[k];
-        base += skipped, c |= (u64)digit << shift;
-      }
-      return c;
-    };
-    // The same among the tokens sent (the barrier that completes them is passed), by CTA 0, which tells the others
-    auto find = [&](int which, int b0, int b1, auto val, u64 target) -> u64 {
-      unsigned most = 0;
-      for (int q = 0; q < R.n; ++q) most = max(most, s_sent[which][q]);
-      if (most > room) return search(b0, b1, val, target);
-      if (R.rank == 0) {
-        const int N = collect(which);
-        auto tell = [&](u64 c) {
-          for (int q = 0; q < R.n; ++q) *cl.map_shared_rank(&s_cut, q) = c;
-        };
-        if (N <= SOLO) {
-          const Mine m = mine_of(N);
-          const bool first = m.at < N && m.part == 0;
-          const u64 w = m.at < N ? val(logit_at(m.place), m.place) : 0;
-          if (first) weights[m.at] = w;
-          __syncthreads();
-          u64 before;
-          int rank;
-          over_others(m, N, [&](u64 x) { return x < m.place; }, before, rank);
-          if (first && before < target && target <= before + w) tell(m.place);
-        } else {
-          R.sort(list, N);
-          constexpr int PER = LIST / THREADS;
-          u64 w[PER], sum = 0, total;
-#pragma unroll
-          for (int j = 0; j < PER; ++j) {
-            const int i = tid * PER + j;
-            w[j] = i < N ? val(logit_at(list[i]), list[i]) : 0, sum += w[j];
-          }
-          u64 before = R.scan_block(sum, total);
-#pragma unroll
-          for (int j = 0; j < PER; ++j) {
-            if (before < target && target <= before + w[j]) tell(list[tid * PER + j]);
-            before += w[j];
-          }
+          for (int k = 0; k < NV; ++k)
+            if (k + 1 == digit) skipped = s[k];
+          base += skipped, c |= (u64)digit << shift;
         }
+        cut = min(cut, c);
       }
-      cl.sync();
-      return s_cut;
-    };
-    if (b_k < BINS) {
-      send(0, b_k, b_k, std::false_type{});
-      cl.sync();
-      cut = find(0, b_k, b_k, [](float, u64) -> u64 { return 1; }, of_b_k);
-    }
-    if (by_p) {
-      if (by_k) bracket();
-      send(1, b_lo, b_hi, std::true_type{});
-      R.sum(sums);
-      const u64 c = find(1, b_lo, b_hi, [&](float z, u64 place) -> u64 { return place <= cut ? weigh(z) : 0; }, times<true>(top_p, sums[0]) - sums[1]);
-      cut = c < cut ? c : cut;
     }
   }
 
-  // ---- the draw: every thread has a run of neighbouring pieces ----
-  auto weight = [&](float z, int v) -> double {
-    const double w = weigh.scaled(z);
-    return w >= least && place_of(z, v) <= cut ? w : 0.0;
-  };
-  const int run = ((n_piece + THREADS - 1) / THREADS) | 1, r_lo = min(n_piece, tid * run), r_hi = min(n_piece, r_lo + run);  // (odd: no bank twice)
+  // ---- the draw: every thread has a run of neighbouring quads ----
+  const int run = ((n_quad + THREADS - 1) / THREADS) | 1, r_lo = min(n_quad, tid * run), r_hi = min(n_quad, r_lo + run);  // (odd: few bank conflicts)
   u64 mine = 0, total;
-  auto add_up = [&](auto all) {
-    for (int i = r_lo; i < r_hi; ++i) {
-      float z[VEC];
-      unpack(z_sm[i], z);
+#pragma unroll 2
+  for (int i = r_lo; i < r_hi; ++i) {
+    const float4 q = quad_of<T>(z_sm, i);
+    const float z[4] = {q.x, q.y, q.z, q.w};
+    double w[4];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        if constexpr (all.value) mine += weigh(z[j]);
-        else mine += Weigher::rounded(weight(z[j], v_lo - head + i * VEC + j));
-      }
+    for (int j = 0; j < 4; ++j) w[j] = weigh.scaled(z[j]);
+    if (cut != ~0ull || least > 0.0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (w[j] < least || place_of(z[j], v_first + i * 4 + j) > cut) w[j] = 0.0;
     }
-  };
-  if (cut == ~0ull && least == 0.0) add_up(std::true_type{});
-  else add_up(std::false_type{});
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mine += Weigher::rounded(w[j]);
+  }
   u64 before = R.scan(mine, total);
   const u64 at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;  // (total is 2^S at least: the largest logit stays)
   if (before <= at && at < before + mine) {
-    const T* zs = reinterpret_cast<const T*>(z_sm);
-    for (int e = r_lo * VEC; e < r_hi * VEC; ++e) {
-      const int v = v_lo - head + e;
-      const double w = weight(to_f32<T>(zs[e]), v);
+#pragma unroll 1
+    for (int e = r_lo * 4; e < r_hi * 4; ++e) {
+      const float z = to_f32<T>(reinterpret_cast<const T*>(z_sm)[e]);
+      const double w = weigh_one(weigh, z);
+      if (w < least || place_of(z, v_first + e) > cut) continue;
       before += Weigher::rounded(w);
       if (before > at) {
-        put(v, (float)(w / (double)total));
+        put(v_first + e, (float)(w / (double)total));
         break;
       }
     }

@@ -95,14 +95,14 @@ bool allow_smem(const void* fn, int bytes, std::atomic<unsigned long long>& done
 // ---- attention behind a shared prefix ----
 struct PxPlan {
   int max_tiles, tc_tiles;
-  size_t plan_off, item_ml, item_o, warp_ml, warp_o, tc_item_ml, tc_item_o, tc_work_ml, tc_work_o, total;
+  size_t state, item_seg, tc_seg, item_ml, item_o, warp_ml, warp_o, tc_item_ml, tc_item_o, tc_work_ml, tc_work_o, total;
 };
 constexpr int PXT_MIN_ROWS = 33;  // rows of the batch and a kv head from which on the prefix goes to the tensor cores' tiles
 bool px_plan(int T, int B, int nq, int nkv, int d, int P, PxPlan* o) {
   if (T < 0 || B < 0 || B > PX_MAX_SEQS || nq < 1 || nkv < 1 || nq % nkv || (d != 64 && d != 128) || P < 0) return false;
   if ((int64_t)T * nq > (1 << 27) || nkv > 65535) return false;
   const int rows = T * (nq / nkv);
-  o->max_tiles = rows / 16 + B + (P > 0 ? rows / 16 + 1 : 0);
+  o->max_tiles = rows / 16 + B + 1 + (P > 0 ? rows / 16 + 1 : 0);
   o->tc_tiles = rows >= PXT_MIN_ROWS && P > 0 ? (rows + PXT_ROWS - 1) / PXT_ROWS : 0;
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -110,7 +110,7 @@ bool px_plan(int T, int B, int nq, int nkv, int d, int P, PxPlan* o) {
     at += (n + 255) / 256 * 256;
     return r;
   };
-  o->plan_off = take((size_t)(2 * (B + 1) + 4) * 4);
+  o->state = take(4), o->item_seg = take((size_t)nkv * o->max_tiles * 8), o->tc_seg = take((size_t)nkv * o->tc_tiles * 8);
   o->item_ml = take((size_t)nkv * o->max_tiles * 128);
   o->item_o = take((size_t)nkv * o->max_tiles * 16 * d * 4);
   o->warp_ml = take((size_t)PX_SMS * PXR_WARPS * 128);
@@ -167,11 +167,11 @@ int px_launch(PrefixParams& p, const PxPlan& t, int dtype, void* stream) {
     (void)cudaGetLastError();
     return LOOPSPEC_ECUDA;
   }
-  // the fold: a CTA per row and query head while there are few, else a warp
-  const int64_t per_seq = ((int64_t)p.T * p.G + p.B - 1) / p.B;
-  if ((int64_t)p.T * p.nq <= 4 * kSms)
-    return launch(prefix_merge_kernel<T, D, 4>, dim3(p.kv.n_kv, p.B, (unsigned)std::min<int64_t>(per_seq, 64)), 128, 0, stream, p, true);
-  return launch(prefix_merge_kernel<T, D, 1>, dim3(p.kv.n_kv, p.B, (unsigned)std::min<int64_t>((per_seq + 3) / 4, 64)), 128, 0, stream, p, true);
+  // the fold: a CTA per sequence and query head while there are few rows, else a warp; long runs of rows over several
+  const int64_t heads = (int64_t)p.B * p.nq;
+  const unsigned y = (unsigned)std::min<int64_t>(64, std::max<int64_t>(1, ((int64_t)p.T * 2 + p.B - 1) / p.B));
+  if ((int64_t)p.T * p.nq <= 4 * kSms) return launch(prefix_merge_kernel<T, D, 4>, dim3((unsigned)heads, y), 128, 0, stream, p, true);
+  return launch(prefix_merge_kernel<T, D, 1>, dim3((unsigned)((heads + 3) / 4), y), 128, 0, stream, p, true);
 }
 
 // ---- sampling ----
@@ -179,7 +179,7 @@ constexpr int SMP_MAX_VOCAB = 1 << 18, SMP_SMEM = 200 * 1024;
 template <typename T>
 int smp_launch(smp::Params& p, void* stream) {
   static std::atomic<unsigned long long> allowed;
-  constexpr int extra = 32 + smp::BINS * 8 + (smp::LIST + smp::SOLO) * 8;
+  constexpr int extra = 32 + smp::BINS * 8 + (smp::LIST + 2 * smp::SOLO) * 8;
   // CTAs per row: as many as the rows leave SMs for (two CTAs share one), none with less than 2048 tokens; more where a slice would not let two CTAs share
   int cs = 1;
   while (cs < smp::MAX_CS && ((p.V > 2048 * cs && p.rows * cs <= kSms) || (p.V / cs) * (int)sizeof(T) + extra > 110 * 1024)) cs *= 2;
@@ -249,7 +249,7 @@ int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t
   p.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)p.kv.d) : scale) * 1.4426950408889634f;
   p.max_tiles = t.max_tiles;
   unsigned char* sc = static_cast<unsigned char*>(scratch);
-  p.plan = reinterpret_cast<int*>(sc + t.plan_off);
+  p.state = reinterpret_cast<int*>(sc + t.state), p.item_seg = reinterpret_cast<int2*>(sc + t.item_seg), p.tc_seg = reinterpret_cast<int2*>(sc + t.tc_seg);
   p.item_ml = reinterpret_cast<float*>(sc + t.item_ml), p.item_o = reinterpret_cast<float*>(sc + t.item_o);
   p.warp_ml = reinterpret_cast<float*>(sc + t.warp_ml), p.warp_o = reinterpret_cast<float*>(sc + t.warp_o);
   p.tc_item_ml = reinterpret_cast<float*>(sc + t.tc_item_ml), p.tc_item_o = reinterpret_cast<float*>(sc + t.tc_item_o);
