@@ -622,20 +622,26 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   // ---- the draw: every thread has a run of neighbouring quads ----
   const int run = ((n_quad + THREADS - 1) / THREADS) | 1, r_lo = min(n_quad, tid * run), r_hi = min(n_quad, r_lo + run);  // (odd: few bank conflicts)
   u64 mine = 0, total;
+  if (cut == ~0ull && least == 0.0) {
 #pragma unroll 2
-  for (int i = r_lo; i < r_hi; ++i) {
-    const float4 q = quad_of<T>(z_sm, i);
-    const float z[4] = {q.x, q.y, q.z, q.w};
-    double w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = weigh.scaled(z[j]);
-    if (cut != ~0ull || least > 0.0) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (w[j] < least || place_of(z[j], v_first + i * 4 + j) > cut) w[j] = 0.0;
+    for (int i = r_lo; i < r_hi; ++i) {
+      const float4 q = quad_of<T>(z_sm, i);
+      mine += (weigh(q.x) + weigh(q.y)) + (weigh(q.z) + weigh(q.w));
     }
+  } else {
+    // mostly few stay: those that rank ahead of the cut, and only then their weights
+    const unsigned key_cut = ~(unsigned)(cut >> MAX_VOCAB_BITS);  // (of no cut: 0)
+#pragma unroll 1
+    for (int i = r_lo; i < r_hi; ++i) {
+      const float4 q = quad_of<T>(z_sm, i);
+      const float z[4] = {q.x, q.y, q.z, q.w};
+      if (max(max(key_of(q.x), key_of(q.y)), max(key_of(q.z), key_of(q.w))) < key_cut) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) mine += Weigher::rounded(w[j]);
+      for (int j = 0; j < 4; ++j) {
+        const double w = weigh.scaled(z[j]);
+        mine += w >= least && place_of(z[j], v_first + i * 4 + j) <= cut ? Weigher::rounded(w) : 0;
+      }
+    }
   }
   u64 before = R.scan(mine, total);
   const u64 at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;  // (total is 2^S at least: the largest logit stays)
