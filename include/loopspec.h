@@ -310,7 +310,7 @@ typedef struct {
  * n_kv_heads key heads, then the value heads.  Rows cu_rows[b] .. cu_rows[b + 1] - 1 (int32 [n_seqs + 1], ascending from 0) are the next tokens of
  * sequence b, which has cached[b] positions already: row j gets position cached[b] + j of page_table[b] (int32, table_width entries, rows table_ld
  * apart).  Rows from cu_rows[n_seqs] on are padding: neither q nor the cache is touched for them.
- * Queries and keys are multiplied by gain / sqrt(mean of the head's squares + eps) where a gain (q_norm, k_norm: fp32 [head_dim], or NULL) is given, then
+ * Queries and keys are multiplied by gain / sqrt(mean of the head's squares + eps) where a gain (q_norm, k_norm: fp32 [head_dim], 16-byte aligned, or NULL) is given, then
  * rotated: pairs (i, i + rot_dim / 2) of the first rot_dim elements turn by index * inv_freq[i] (fp64 [rot_dim / 2], radians per position;
  * rot_dim % 8 == 0, 0 = no rotation), index = position + pos_offset[b] (int32 [n_seqs], NULL = 0: the length of a shared prefix, say).  The angle is taken
  * in 64 bits, the rest in fp32 and rounded once to the cache's type; q_out: [T] rows of n_q_heads heads of that type, q_ld elements apart

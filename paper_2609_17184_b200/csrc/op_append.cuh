@@ -29,36 +29,52 @@ struct AppendParams {
   long long table_ld;    // elements from a row of the table to the next
   int table_w;
   int T, B, nq, rot;
+  int row_warps;          // warps of a CTA that share a row's heads: all of them, or 1
   int* err;
 };
 
+// four elements as they come
 template <typename T>
-__device__ __forceinline__ void app_load4(const T* p, float (&v)[4]) {
-  if constexpr (sizeof(T) == 4) {
-    const float4 w = __ldcs(reinterpret_cast<const float4*>(p));
-    v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
-  } else {
-    const uint2 w = __ldcs(reinterpret_cast<const uint2*>(p));
+struct AppRaw {
+  uint2 w;
+  __device__ __forceinline__ void load(const T* p) { w = __ldcs(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void get(float (&v)[4]) const {
     const T* e = reinterpret_cast<const T*>(&w);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = to_f32<T>(e[i]);
   }
-}
+};
+template <>
+struct AppRaw<float> {
+  float4 w;
+  __device__ __forceinline__ void load(const float* p) { w = __ldcs(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w; }
+};
 
 // LH: lanes per head (a power of two >= d / 8)
 template <typename TI, typename TO, int LH>
 __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_constant__ AppendParams p) {
-  constexpr int HPW = 32 / LH;  // heads a warp works on at once
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x;
+  constexpr int HPW = 32 / LH;                  // heads a warp works on at once
+  constexpr int AHEAD = sizeof(TI) == 4 ? 2 : 3;  // such turns in flight: the look-ups below are a chain of four reads, and a row is over after a few turns
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row = p.row_warps == 1 ? blockIdx.x * APP_WARPS + warp : blockIdx.x, part = p.row_warps == 1 ? 0 : warp;
+  if (row >= p.T) return;
   const int d = p.kv.d, n_heads = p.nq + 2 * p.kv.n_kv;
-  const int c = lane & (LH - 1), step = gridDim.y * APP_WARPS * HPW;
-  int h = (blockIdx.y * APP_WARPS + warp) * HPW + lane / LH;
+  const int c = lane & (LH - 1), step = gridDim.y * p.row_warps * HPW;
+  const int h_warp = (blockIdx.y * p.row_warps + part) * HPW, h_lane = lane / LH;
   const bool live = c < d / 8, turns = 8 * c < p.rot;
   // this lane's elements: i0 .. i0 + 3 and i1 .. i1 + 3 of a head
   const int c0 = turns ? 4 * c : p.rot + 4 * (c - p.rot / 8), i0 = live ? c0 : 0, i1 = live ? i0 + (turns ? p.rot : d - p.rot) / 2 : 0;
   const TI* x = static_cast<const TI*>(p.qkv) + (long long)row * p.ld;
-  float a[4], b[4];
-  if (h < n_heads) app_load4(x + h * d + i0, a), app_load4(x + h * d + i1, b);  // (requested ahead of the look-ups)
+  AppRaw<TI> ra[AHEAD], rb[AHEAD];
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) {
+      const int h = h0 + t * step + h_lane;
+      if (h < n_heads) ra[t].load(x + h * d + i0), rb[t].load(x + h * d + i1);
+    }
+  };
+  fetch(h_warp);
 
   const int seq = seq_of_row(p.cu_rows, p.B, row, lane);
   if (seq < 0 || row >= __ldg(p.cu_rows + seq + 1)) return;  // behind the last sequence: left as it was
@@ -67,7 +83,7 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
   int page = -1;
   if (pos >= 0 && pg < p.table_w) page = __ldg(p.page_table + seq * p.table_ld + pg);
   const bool ok = page >= 0 && page < p.kv.n_pages;
-  if (!ok && p.err && threadIdx.x == 0 && blockIdx.y == 0) atomicOr(p.err, OP_BAD_PAGE);
+  if (!ok && p.err && lane == 0) atomicOr(p.err, OP_BAD_PAGE);
   const long long slot = pos & ((1ll << p.kv.page_shift) - 1);
   const long long at = (long long)page * p.kv.page_stride + slot * p.kv.slot_stride;
 
@@ -81,31 +97,35 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
       sincospif(2.f * (float)t, &sn[i], &cs[i]);
     }
   }
-  float gq[8], gk[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    gq[i] = p.q_norm ? __ldg(p.q_norm + i0 + i) : 1.f, gq[4 + i] = p.q_norm ? __ldg(p.q_norm + i1 + i) : 1.f;
-    gk[i] = p.k_norm ? __ldg(p.k_norm + i0 + i) : 1.f, gk[4 + i] = p.k_norm ? __ldg(p.k_norm + i1 + i) : 1.f;
-  }
   const float inv_d = 1.f / (float)d;
   // (the trip count is the warp's: its lanes shuffle together)
-  for (int h0 = (blockIdx.y * APP_WARPS + warp) * HPW; h0 < n_heads; h0 += step, h += step) {
-    float na[4], nb[4];
-    const bool more = h + step < n_heads;
-    if (more) app_load4(x + (h + step) * d + i0, na), app_load4(x + (h + step) * d + i1, nb);
-    const bool is_q = h < p.nq, is_k = !is_q && h < p.nq + p.kv.n_kv, is_v = !is_q && !is_k;
-    const bool norm = is_q ? p.q_norm != nullptr : is_k && p.k_norm != nullptr;
-    float ss = 0.f;
-    if (live && h < n_heads)
+  for (int h0 = h_warp; h0 < n_heads; h0 += AHEAD * step) {
+    float va[AHEAD][4], vb[AHEAD][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ss += a[i] * a[i] + b[i] * b[i];
+    for (int t = 0; t < AHEAD; ++t) ra[t].get(va[t]), rb[t].get(vb[t]);
+    if (h0 + AHEAD * step < n_heads) fetch(h0 + AHEAD * step);
 #pragma unroll
-    for (int o = LH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (live && h < n_heads) {
-      if (norm) {
-        const float r = 1.f / sqrtf(ss * inv_d + p.eps);
+    for (int t = 0; t < AHEAD; ++t) {
+      if (h0 + t * step >= n_heads) break;
+      float(&a)[4] = va[t], (&b)[4] = vb[t];
+      const int h = h0 + t * step + h_lane;
+      const bool is_q = h < p.nq, is_k = !is_q && h < p.nq + p.kv.n_kv, is_v = !is_q && !is_k;
+      const float* gain = is_q ? p.q_norm : is_k ? p.k_norm : nullptr;
+      if (!live || h >= n_heads)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = a[i] * r * (is_q ? gq[i] : gk[i]), b[i] = b[i] * r * (is_q ? gq[4 + i] : gk[4 + i]);
+        for (int i = 0; i < 4; ++i) a[i] = b[i] = 0.f;
+      if (p.q_norm || p.k_norm) {
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ss += a[i] * a[i] + b[i] * b[i];
+#pragma unroll
+        for (int o = LH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        if (gain) {
+          const float r = rsqrtf(ss * inv_d + p.eps);  // (2 ulp)
+          const float4 g0 = *reinterpret_cast<const float4*>(gain + i0), g1 = *reinterpret_cast<const float4*>(gain + i1);
+          a[0] *= r * g0.x, a[1] *= r * g0.y, a[2] *= r * g0.z, a[3] *= r * g0.w;
+          b[0] *= r * g1.x, b[1] *= r * g1.y, b[2] *= r * g1.z, b[3] *= r * g1.w;
+        }
       }
       if (turns && !is_v) {
 #pragma unroll
@@ -117,13 +137,11 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
       TO* dst = nullptr;
       if (is_q) dst = static_cast<TO*>(p.q) + (long long)row * p.q_ld + h * d;
       else if (ok) dst = static_cast<TO*>(is_k ? p.kv.k : p.kv.v) + at + (long long)(h - p.nq - (is_k ? 0 : p.kv.n_kv)) * p.kv.head_stride;
-      if (dst) {
+      if (dst && live && h < n_heads) {
         *reinterpret_cast<uint2*>(dst + i0) = make_uint2(pack2<TO>(a[0], a[1]), pack2<TO>(a[2], a[3]));
         *reinterpret_cast<uint2*>(dst + i1) = make_uint2(pack2<TO>(b[0], b[1]), pack2<TO>(b[2], b[3]));
       }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = na[i], b[i] = nb[i];
   }
 }
 

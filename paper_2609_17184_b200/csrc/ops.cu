@@ -201,6 +201,7 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
   AppendParams p;
   memset(&p, 0, sizeof p);
   if (!paged_kv(kv, &p.kv) || qkv_dtype < 0 || qkv_dtype > 2 || T < 0 || n_seqs < 0 || n_q_heads < 0 || n_q_heads > 65536 || p.kv.n_kv > 65536) return LOOPSPEC_EINVAL;
+  if ((q_norm && !aligned16(q_norm)) || (k_norm && !aligned16(k_norm))) return LOOPSPEC_EINVAL;
   if (rot_dim < 0 || rot_dim > p.kv.d || rot_dim % 8 || (rot_dim && !inv_freq)) return LOOPSPEC_EINVAL;
   if (table_width < 0 || table_ld < table_width) return LOOPSPEC_EINVAL;
   if (T == 0 || n_seqs == 0) return LOOPSPEC_OK;  // (every row is padding)
@@ -214,10 +215,13 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
   int lh = 1;
   while (lh < p.kv.d / 8) lh *= 2;
   const AppendFn fn = kv->dtype == 1 ? append_fn<__nv_bfloat16>(qkv_dtype, lh) : append_fn<__half>(qkv_dtype, lh);
-  // few rows: a row's heads over several CTAs
-  const int per_cta = APP_WARPS * (32 / lh), iters = (int)((n_q_heads + 2 * (int64_t)p.kv.n_kv + per_cta - 1) / per_cta);
-  const int split = std::max(1, std::min(iters, 1184 / T));
-  return launch(fn, dim3(T, split), APP_WARPS * 32, 0, cuda_stream, p);
+  // Few rows: a row's heads over the warps of several CTAs, for what counts is the way to the last store.  Many: a warp per row, so that look-ups and sines
+  // are taken once for all heads [us with all warps / with one, 48 heads of 128 with norms: 8000 rows 50 / 44, 2000 14.8 / 15.1, 1000 9.5 / 12.2, 200 5.4 /
+  // 11; 48 heads of 64 without: 8000 29 / 19, 2000 8.9 / 7.2, 1000 6.0 / 5.9].
+  p.row_warps = T >= 2000 ? 1 : APP_WARPS;
+  const int per_turn = p.row_warps * (32 / lh), turns = (int)((n_q_heads + 2 * (int64_t)p.kv.n_kv + per_turn - 1) / per_turn);
+  const int split = p.row_warps == 1 ? 1 : std::max(1, std::min(turns, 1184 / T));
+  return launch(fn, dim3(p.row_warps == 1 ? (T + APP_WARPS - 1) / APP_WARPS : T, split), APP_WARPS * 32, 0, cuda_stream, p);
 }
 
 size_t loopspec_prefix_attention_scratch_bytes(int32_t T, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t prefix_len) {

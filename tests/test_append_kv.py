@@ -86,6 +86,8 @@ CASES = [
     ([2, 3], [0, 8], 0, 2, 64, 16, "fp32", "bf16", 64, True, 0, None),
     ([1, 2], [10, 0], 32, 8, 128, 16, "fp32", "bf16", 128, True, 0, [1000003, 2 ** 30]),
     ([2, 1] * 700, [0, 1] * 700, 2, 1, 16, 2, "fp32", "bf16", 16, False, 7, None),
+    ([1100, 0, 1299], [5, 7, 0], 3, 2, 64, 32, "bf16", "bf16", 32, True, 3, None),  # a warp per row
+    ([2050], [1], 2, 1, 40, 16, "fp32", "fp16", 40, False, 1, [3]),
 ]
 
 
@@ -226,6 +228,9 @@ def test_refusals():
                dict(cu_=None), dict(B=-1), dict(f=None), dict(rot=12), dict(rot=72), dict(rot=-8), dict(q=None), dict(q=A + 8), dict(qld=120), dict(qld=132),
                dict(x=None), dict(x=A + 8)):
         assert rc(**kw) == -1, kw
+    for qn, kn in ((A + 4, None), (None, A + 8)):
+        kv = PagedKv(*ok())
+        assert ls.lib.loopspec_op_append_kv(A, 1, 256, 2, 2, C.byref(kv), A, 4, 4, A, A, 1, None, A, 64, qn, kn, 1e-6, A, 128, None, None) == -1
     assert ls.lib.loopspec_op_append_kv(A, 1, 256, 2, 2, None, A, 4, 4, A, A, 1, None, A, 64, None, None, 1e-6, A, 128, None, None) == -1
     assert rc(T=0) == 0 and rc(B=0) == 0  # nothing to do
 
