@@ -13,7 +13,10 @@
 // of small pages is 32 requests of a warp at once), 128-byte swizzle: K as a K-major operand, V - rows of keys - as an MN-major one.
 //
 // What bounds it: at head size 128 the two products of a tile take 1024 cycles at best (both operands of the first come from shared memory, which
-// 128 x 128 tiles saturate) and its 16,384 exponentials, at 16 a cycle, as many; a quarter of them are taken by a polynomial instead.
+// 128 x 128 tiles saturate) and its 16,384 exponentials, at 16 a cycle, as many.  It takes 1570: a stream's tile is a chain of about 3100 (scores
+// 100, their read 250, maximum 500, reference 500, weights 1400, hand-over), and there are two streams.  384 rows of 16 heads against 16,384 keys
+// take 63 us, 0.8 PFLOP/s.  Measured and left out: a quarter of the exponentials by a polynomial on the FMA pipe (no change; half: 5 %
+// slower), two threads per row (no change).
 #pragma once
 #include "op_attention.cuh"
 
@@ -56,32 +59,6 @@ __device__ __forceinline__ float pxt_max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-__device__ __forceinline__ unsigned long long pxt_mul2(unsigned long long a, unsigned long long b) {
-  unsigned long long r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ float pxt_max_nan(float a, float b) {  // no number stays none
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
-// 2^x of two values up to 2^8: x = k + f, |f| <= 1/2, 2^f by the polynomial of degree 4 with the least relative error there (2.7e-6, fitted by
-// reweighted least squares: a hundredth of the rounding of a weight), times 2^k.  Below -126: 2^-126 (nothing, beside 1).
-__device__ __forceinline__ unsigned long long pxt_exp2_poly(unsigned long long x) {
-  float a, b;
-  pxt_split(x, a, b);
-  x = pxt_two(pxt_max_nan(a, -126.f), pxt_max_nan(b, -126.f));
-  const float magic = 12582912.f;  // 1.5 * 2^23: the sum's low bits are x to the nearest integer
-  const unsigned long long t = pxt_add2(x, pxt_two(magic, magic));
-  const unsigned long long f = pxt_fma2(pxt_add2(t, pxt_two(-magic, -magic)), pxt_two(-1.f, -1.f), x);
-  unsigned long long q = pxt_fma2(pxt_two(0.009570102207362652f, 0.009570102207362652f), f, pxt_two(0.05591785907745361f, 0.05591785907745361f));
-  q = pxt_fma2(q, f, pxt_two(0.240247443318367f, 0.240247443318367f));
-  q = pxt_fma2(q, f, pxt_two(0.6931217908859253f, 0.6931217908859253f));
-  q = pxt_fma2(q, f, pxt_two(0.9999992847442627f, 0.9999992847442627f));
-  pxt_split(t, a, b);
-  return pxt_mul2(q, pxt_two(__uint_as_float((__float_as_uint(a) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(b) << 23) + 0x3f800000u)));
 }
 __device__ __forceinline__ void pxt_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void pxt_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -345,16 +322,10 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
         unsigned wt[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          unsigned long long x = pxt_fma2(pxt_two(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), sc2, sub2);
           float a, b;
-          if (e % 4 == 3) {
-            x = pxt_exp2_poly(x);
-            pxt_split(x, a, b);
-          } else {
-            pxt_split(x, a, b);
-            a = px_exp2(a), b = px_exp2(b), x = pxt_two(a, b);
-          }
-          sum[e & 1] = pxt_add2(sum[e & 1], x);
+          pxt_split(pxt_fma2(pxt_two(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), sc2, sub2), a, b);
+          a = px_exp2(a), b = px_exp2(b);
+          sum[e & 1] = pxt_add2(sum[e & 1], pxt_two(a, b));
           wt[e] = pack2<T>(a, b);
         }
         pxt_st16(t_p + 16 * c, wt);
