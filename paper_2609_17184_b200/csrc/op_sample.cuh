@@ -238,7 +238,7 @@ struct Cluster {
 
 // four neighbouring logits of a slice
 template <typename T>
-__device__ __forceinline__ float4 quad_of(const void* z_sm, int i) {
+__device__ __forceinline__ float4 quad_of(const T* z_sm, int i) {
   if constexpr (sizeof(T) == 4) {
     return reinterpret_cast<const float4*>(z_sm)[i];
   } else {
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   const T* src = static_cast<const T*>(p.logits) + row * p.ld + v_lo;
   const int head = (int)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));  // elements from the 16-byte boundary before the slice
   const int n_piece = (head + n + VEC - 1) / VEC, whole = (head + n) / VEC, n_quad = n_piece * (VEC / 4), v_first = v_lo - head;
-  unsigned char* z_sm = smp_smem;  // element e: token v_first + e
+  T* z_sm = reinterpret_cast<T*>(smp_smem);  // element e: token v_first + e
   float top = -INFINITY;
   {
     const uint4* vs = reinterpret_cast<const uint4*>(src - head);
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     const int e = tid < VEC ? tid : whole * VEC + tid - VEC;  // the first piece's and the last one's elements
     if (tid < VEC ? head != 0 || whole == 0 : tid < 2 * VEC && whole < n_piece && (whole > 0 || head == 0)) {
       const T z = e >= head && e < head + n ? src[e - head] : T(-INFINITY);
-      reinterpret_cast<T*>(z_sm)[e] = z, top = fmaxf(top, to_f32<T>(z));
+      z_sm[e] = z, top = fmaxf(top, to_f32<T>(z));
     }
   }
   if (tid < 256) s_table[tid] = exp2((double)tid / 256);
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     unsigned first = 0;
 #pragma unroll 1
     for (int i = tid; i < n_quad; i += THREADS) {
-      const float4 q = quad_of<T>(z_sm, i);
+      const float4 q = quad_of(z_sm, i);
       const int j = q.x == top ? 0 : q.y == top ? 1 : q.z == top ? 2 : q.w == top ? 3 : 4;
       if (j < 4) first = max(first, 0x7fffffffu - (unsigned)(v_first + i * 4 + j));
     }
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     __syncthreads();
 #pragma unroll 2
     for (int i = tid; i < n_quad; i += THREADS) {
-      const float4 q = quad_of<T>(z_sm, i);
+      const float4 q = quad_of(z_sm, i);
       const float z[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         const float f0 = (float)b_lo, f1 = (float)(b_hi + 1);  // (b_hi < BINS)
 #pragma unroll 2
         for (int i = tid; i < n_quad; i += THREADS) {
-          const float4 q = quad_of<T>(z_sm, i);
+          const float4 q = quad_of(z_sm, i);
           const float z[4] = {q.x, q.y, q.z, q.w};
           if (mass) {
             u64 w[4];
@@ -595,7 +595,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
           for (int k = 0; k < NV; ++k) s[k] = 0;
 #pragma unroll 1
           for (int e = tid; e < n_quad * 4; e += THREADS) {
-            const float z = to_f32<T>(reinterpret_cast<const T*>(z_sm)[e]), d = depth_of(z);
+            const float z = to_f32<T>(z_sm[e]), d = depth_of(z);
             const u64 place = place_of(z, v_first + e);
             if (!(d >= (float)b_lo && d < (float)(b_hi + 1)) || place >> (shift + 3) != c >> (shift + 3)) continue;
             const u64 x = k_cut ? 1 : place <= cut ? Weigher::rounded(weigh_one(weigh, z)) : 0;
@@ -619,43 +619,63 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     }
   }
 
-  // ---- the draw: every thread has a run of neighbouring quads ----
-  const int run = ((n_quad + THREADS - 1) / THREADS) | 1, r_lo = min(n_quad, tid * run), r_hi = min(n_quad, r_lo + run);  // (odd: few bank conflicts)
+  // ---- the draw: every warp has a run of neighbouring quads, its lanes take them in turn ----
+  const int lane = tid & 31, run = ((n_quad + THREADS - 1) / THREADS) * 32, r_lo = min(n_quad, (tid >> 5) * run), r_hi = min(n_quad, r_lo + run);
+  const unsigned key_cut = ~(unsigned)(cut >> MAX_VOCAB_BITS);  // (of no cut: 0)
+  const bool every = cut == ~0ull && least == 0.0;
+  auto few_of = [&](int i) -> u64 {  // mostly few stay: those that rank ahead of the cut, and only then their weights
+    const float4 q = quad_of(z_sm, i);
+    if (max(max(key_of(q.x), key_of(q.y)), max(key_of(q.z), key_of(q.w))) < key_cut) return 0;
+    const float z[4] = {q.x, q.y, q.z, q.w};
+    u64 sum = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const double w = weigh.scaled(z[j]);
+      sum += w >= least && place_of(z[j], v_first + i * 4 + j) <= cut ? Weigher::rounded(w) : 0;
+    }
+    return sum;
+  };
   u64 mine = 0, total;
-  if (cut == ~0ull && least == 0.0) {
+  if (every) {
 #pragma unroll 2
-    for (int i = r_lo; i < r_hi; ++i) {
-      const float4 q = quad_of<T>(z_sm, i);
+    for (int i = r_lo + lane; i < r_hi; i += 32) {
+      const float4 q = quad_of(z_sm, i);
       mine += (weigh(q.x) + weigh(q.y)) + (weigh(q.z) + weigh(q.w));
     }
   } else {
-    // mostly few stay: those that rank ahead of the cut, and only then their weights
-    const unsigned key_cut = ~(unsigned)(cut >> MAX_VOCAB_BITS);  // (of no cut: 0)
 #pragma unroll 1
-    for (int i = r_lo; i < r_hi; ++i) {
-      const float4 q = quad_of<T>(z_sm, i);
-      const float z[4] = {q.x, q.y, q.z, q.w};
-      if (max(max(key_of(q.x), key_of(q.y)), max(key_of(q.z), key_of(q.w))) < key_cut) continue;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const double w = weigh.scaled(z[j]);
-        mine += w >= least && place_of(z[j], v_first + i * 4 + j) <= cut ? Weigher::rounded(w) : 0;
-      }
-    }
+    for (int i = r_lo + lane; i < r_hi; i += 32) mine += few_of(i);
   }
   u64 before = R.scan(mine, total);
   const u64 at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;  // (total is 2^S at least: the largest logit stays)
-  if (before <= at && at < before + mine) {
+  const u64 end = __shfl_sync(0xffffffffu, before + mine, 31);
+  before = __shfl_sync(0xffffffffu, before, 0);
+  if (before <= at && at < end) {  // in this warp's run
 #pragma unroll 1
-    for (int e = r_lo * 4; e < r_hi * 4; ++e) {
-      const float z = to_f32<T>(reinterpret_cast<const T*>(z_sm)[e]);
-      const double w = weigh_one(weigh, z);
-      if (w < least || place_of(z, v_first + e) > cut) continue;
-      before += Weigher::rounded(w);
-      if (before > at) {
-        put(v_first + e, (float)(w / (double)total));
-        break;
+    for (int i = r_lo + lane; i - lane < r_hi; i += 32) {
+      const u64 x = i < r_hi ? few_of(i) : 0;
+      u64 upto = before + x;  // ... and the lanes' before this one
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 t = __shfl_up_sync(0xffffffffu, upto - before, o);
+        if (lane >= o) upto += t;
       }
+      if (upto - x <= at && at < upto) {
+        u64 sum = upto - x;
+#pragma unroll 1
+        for (int e = i * 4; e < i * 4 + 4; ++e) {
+          const float z = to_f32<T>(z_sm[e]);
+          const double w = weigh_one(weigh, z);
+          if (w < least || place_of(z, v_first + e) > cut) continue;
+          sum += Weigher::rounded(w);
+          if (sum > at) {
+            put(v_first + e, (float)(w / (double)total));
+            break;
+          }
+        }
+      }
+      before = __shfl_sync(0xffffffffu, upto, 31);
+      if (before > at) break;
     }
   }
 }

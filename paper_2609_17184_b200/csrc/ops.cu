@@ -180,9 +180,10 @@ template <typename T>
 int smp_launch(smp::Params& p, void* stream) {
   static std::atomic<unsigned long long> allowed;
   constexpr int extra = 32 + smp::BINS * 8 + (smp::LIST + 2 * smp::SOLO) * 8;
-  // CTAs per row: as many as the rows leave SMs for (two CTAs share one), none with less than 2048 tokens; more where a slice would not let two CTAs share
+  // CTAs per row: up to three for every two SMs (two share one; a cluster's hand-overs cost more than a wider one gains: 64 rows of 32,000 take 15 us
+  // with two each, 18 with four), none with less than 2048 tokens; more where a slice would not fit
   int cs = 1;
-  while (cs < smp::MAX_CS && ((p.V > 2048 * cs && p.rows * cs <= kSms) || (p.V / cs) * (int)sizeof(T) + extra > 110 * 1024)) cs *= 2;
+  while (cs < smp::MAX_CS && ((p.V > 2048 * cs && p.rows * cs * 2 <= kSms * 3 / 2) || (p.V / cs + 8) * (int)sizeof(T) + extra > SMP_SMEM)) cs *= 2;
   p.per = ((p.V + cs - 1) / cs + 7) / 8 * 8;
   p.hist_off = p.per * (int)sizeof(T) + 32;  // (a piece more than the slice: it need not begin on a boundary)
   const int bytes = p.hist_off - 32 + extra;
