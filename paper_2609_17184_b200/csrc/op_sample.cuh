@@ -29,6 +29,7 @@ constexpr int BINS = 2 * THREADS;  // of the distance from the best logit, as fa
 constexpr int LIST = 2048;         // tokens one CTA can be sent, an equal part of them by each CTA
 constexpr int SOLO = 256;          // candidates with which one CTA finishes a row alone
 static_assert(2 * SOLO == THREADS, "the list's companion holds a pair for each of them, or a sum for each thread");
+constexpr int QUICK = 192;         // top-k times CTAs of a row up to which that is tried without a histogram
 constexpr int MAX_VOCAB_BITS = 18;
 
 struct Params {
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   __shared__ double s_table[256];
   __shared__ u64 s_sh[WARPS * NV], s_part[2 * MAX_CS * NV], s_before[3], s_upto, s_cut;
   __shared__ int s_found[3];
-  __shared__ unsigned s_mine[2], s_sent[2][MAX_CS];  // tokens this CTA has sent, and what every CTA has, for either cut
+  __shared__ unsigned s_mine[3], s_sent[3][MAX_CS];  // tokens this CTA has sent, and what every CTA has, each time
   cg::cluster_group cl = cg::this_cluster();
   Cluster R{cl, (int)cl.num_blocks(), (int)cl.block_rank(), 0, s_sh, s_part};
   const int tid = threadIdx.x, row = blockIdx.x / R.n, V = p.V;
@@ -291,6 +292,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     }
   }
   if (tid < 256) s_table[tid] = exp2((double)tid / 256);
+  const float own_top = top;
   const unsigned top_key = (unsigned)R.max(key_of(top));
   top = logit_of(top_key);
   auto put = [&](int token, float prob) {
@@ -335,32 +337,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
       const float d = (z == top ? 0.f : top - z) * scale;
       return z > weigh.none ? d : (float)BINS;
     };
-    for (int i = tid; i < BINS / 2; i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) s_cut = ~0ull, s_mine[0] = s_mine[1] = 0, s_found[0] = s_found[1] = s_found[2] = BINS;
-    __syncthreads();
-#pragma unroll 2
-    for (int i = tid; i < n_quad; i += THREADS) {
-      const float4 q = quad_of(z_sm, i);
-      const float z[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float d = depth_of(z[j]);
-        if (d < (float)BINS) {
-          const int b = (int)d;
-          atomicAdd(hist + b, 1u);
-          if (by_p) atomicAdd(hist + BINS + b, (unsigned)((d - (float)b) * 1024.f));
-        }
-      }
-    }
-    cl.sync();
-    // this thread's two bins in the whole cluster
-    u64 cnt[2] = {0, 0}, low[2] = {0, 0};
-#pragma unroll 8
-    for (int q = 0; q < R.n; ++q) {
-      const unsigned* h = cl.map_shared_rank(hist, q) + 2 * tid;
-      const uint2 c = *reinterpret_cast<const uint2*>(h), l = *reinterpret_cast<const uint2*>(h + BINS);
-      cnt[0] += c.x, cnt[1] += c.y, low[0] += l.x, low[1] += l.y;
-    }
+    if (tid == 0) s_cut = ~0ull, s_mine[0] = s_mine[1] = s_mine[2] = 0, s_found[0] = s_found[1] = s_found[2] = BINS;
     // the first bin at whose end the sum of w over the bins reaches target: s_found[slot]; the sum before it: s_before[slot]
     auto crossing = [&](u64 before, u64 w0, u64 w1, u64 target, int slot) {
       if (before < target && target <= before + w0 + w1) {
@@ -368,24 +345,64 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         s_found[slot] = 2 * tid + second, s_before[slot] = before + (second ? w0 : 0);
       }
     };
-    u64 n_all;
-    const u64 n_before = R.scan_block(cnt[0] + cnt[1], n_all);  // tokens of the bins above this thread's
-    int b_k = BINS;      // the bin where top-k cuts, and how many of it stay
-    u64 of_b_k = 0;
-    if (by_k) {
-      crossing(n_before, cnt[0], cnt[1], top_k, 0);
-      __syncthreads();
-      b_k = s_found[0];
-      if (b_k < BINS) of_b_k = top_k - s_before[0];
-    }
     const unsigned room = LIST / R.n;
     bool solo = false;
     u64 all = 0;  // the mass top-p is a part of
-    // First top-k (or, where few tokens are candidates at all, whatever cuts there are), then top-p
+    u64 cnt[2] = {0, 0}, low[2] = {0, 0}, n_before = 0, n_all;  // this thread's two bins in the whole cluster, and tokens of the bins above them
+    int b_k = BINS;                                             // the bin where top-k cuts, and how many of it stay
+    u64 of_b_k = 0;
+    // First top-k (or, where few tokens are candidates at all, whatever cuts there are), then top-p.  Before that, for a small k: at least k tokens reach
+    // the k-th largest of the threads' own maxima, and mostly not many more; if they are as few as that, no histogram of all tokens is needed.
 #pragma unroll 1
-    for (int step_ = 0; step_ < 2; ++step_) {
+    for (int step_ = by_k && top_k * R.n <= QUICK ? -1 : 0; step_ < 2; ++step_) {
       int b_lo = 0, b_hi = BINS - 1;
-      if (by_p && by_k == (step_ == 1)) {
+      if (step_ <= 0) {
+        for (int i = tid; i < BINS / 2; i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        if (step_ < 0) {
+          const float d = depth_of(own_top);
+          if (d < (float)BINS) atomicAdd(hist + (int)d, 1u);
+          __syncthreads();
+          const uint2 c = *reinterpret_cast<const uint2*>(hist + 2 * tid);
+          crossing(R.scan_block(c.x + c.y, n_all), c.x, c.y, top_k, 0);
+          __syncthreads();
+          b_hi = min(s_found[0], BINS - 1);
+          solo = true;
+        } else {
+          solo = false;
+#pragma unroll 2
+          for (int i = tid; i < n_quad; i += THREADS) {
+            const float4 q = quad_of(z_sm, i);
+            const float z[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float d = depth_of(z[j]);
+              if (d < (float)BINS) {
+                const int b = (int)d;
+                atomicAdd(hist + b, 1u);
+                if (by_p) atomicAdd(hist + BINS + b, (unsigned)((d - (float)b) * 1024.f));
+              }
+            }
+          }
+          cl.sync();
+#pragma unroll 8
+          for (int q = 0; q < R.n; ++q) {
+            const unsigned* h = cl.map_shared_rank(hist, q) + 2 * tid;
+            const uint2 c = *reinterpret_cast<const uint2*>(h), l = *reinterpret_cast<const uint2*>(h + BINS);
+            cnt[0] += c.x, cnt[1] += c.y, low[0] += l.x, low[1] += l.y;
+          }
+          n_before = R.scan_block(cnt[0] + cnt[1], n_all);
+          if (by_k) {
+            if (tid == 0) s_found[0] = BINS;
+            __syncthreads();
+            crossing(n_before, cnt[0], cnt[1], top_k, 0);
+            __syncthreads();
+            b_k = s_found[0];
+            if (b_k < BINS) of_b_k = top_k - s_before[0];
+          }
+        }
+      }
+      if (by_p && step_ >= 0 && by_k == (step_ == 1)) {
         // Bins between which top-p cuts.  Weights of a bin of c tokens and summed depths D (in bins; c / 1024 may be missing): with r = 2^-step, at
         // depth x of it r^x <= 1 - x (1 - r) (chord) and r^x >= 1 + x ln r (tangent), times the weight at the bin's upper end.
         u64 up[2], down[2];
@@ -410,7 +427,8 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
         __syncthreads();
         b_lo = min(s_found[1], BINS - 1), b_hi = min(s_found[2], min(b_k, BINS - 1));
       }
-      if (step_ == 0) {
+      if (step_ < 0) {
+      } else if (step_ == 0) {
         const int b_end = by_k ? min(b_k, BINS - 1) : b_hi;
         if (2 * tid == (b_end & ~1)) s_upto = n_before + cnt[0] + (b_end & 1 ? cnt[1] : 0);
         __syncthreads();
@@ -421,7 +439,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
       } else if (!by_p || !by_k) {
         break;  // (found in the first turn)
       }
-      const bool k_cut = by_k && step_ == 0, mass = by_p && !k_cut;
+      const bool k_cut = by_k && step_ <= 0, mass = by_p && !k_cut;
       // ---- this CTA's tokens of the bins b_lo .. b_hi go, in no order, to its part of CTA 0's list, and their number to all; with `mass`, also: the exact weight
       // of what is kept so far, and the part of it in the bins before b_lo ----
       u64 sums[2] = {0, 0};
@@ -442,22 +460,24 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
               sums[0] += w[j], sums[1] += depth_of(z[j]) < f0 ? w[j] : 0;
             }
           }
+          if (!(depth_of(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]))) < f1)) continue;  // (the nearest of the four)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float d = depth_of(z[j]);
             if (d >= f0 && d < f1) {
-              const unsigned at = atomicAdd(s_mine + step_, 1u);
+              const unsigned at = atomicAdd(s_mine + step_ + 1, 1u);
               if (at < room) to[at] = place_of(z[j], v_first + i * 4 + j);
             }
           }
         }
         __syncthreads();
-        if (tid < R.n) *cl.map_shared_rank(&s_sent[step_][R.rank], tid) = s_mine[step_];
+        if (tid < R.n) *cl.map_shared_rank(&s_sent[step_ + 1][R.rank], tid) = s_mine[step_ + 1];
       }
       R.sum(sums);  // (and what was sent has arrived)
       if (mass) all = sums[0];
-      unsigned most = 0;
-      for (int q = 0; q < R.n; ++q) most = max(most, s_sent[step_][q]);
+      unsigned most = 0, of_all = 0;
+      for (int q = 0; q < R.n; ++q) most = max(most, s_sent[step_ + 1][q]), of_all += s_sent[step_ + 1][q];
+      if (step_ < 0 && (most > room || of_all > SOLO)) continue;
       const u64 target = k_cut ? of_b_k : times<true>(top_p, all) - sums[1];
       if (most <= room) {
         if (R.rank == 0) {
@@ -470,12 +490,12 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
             for (int j = 0; j < LIST / THREADS; ++j) {
               const int i = tid + j * THREADS, q = i / (int)room, k = i - q * (int)room;
               e[j] = list[i], at[j] = -1;
-              if (q < R.n && k < (int)s_sent[step_][q]) {
+              if (q < R.n && k < (int)s_sent[step_ + 1][q]) {
                 at[j] = k;
-                for (int x = 0; x < q; ++x) at[j] += s_sent[step_][x];
+                for (int x = 0; x < q; ++x) at[j] += s_sent[step_ + 1][x];
               }
             }
-            for (int q = 0; q < R.n; ++q) N += s_sent[step_][q];
+            for (int q = 0; q < R.n; ++q) N += s_sent[step_ + 1][q];
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < LIST / THREADS; ++j)
