@@ -103,6 +103,33 @@ def test_cuts_that_leave_thousands_of_tokens(V, dt, spread):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,V,dt", [(1, 50001, "fp32"), (20, 20011, "bf16"), (40, 9000, "fp16"), (160, 5003, "fp32"), (300, 700, "bf16")])
+def test_a_small_k_wherever_its_tokens_lie(rows, V, dt):
+    """The largest logits spread, side by side, at either end, many alike, or fewer that weigh anything than k."""
+    rng = np.random.default_rng(V + rows)
+    z = rng.standard_normal((rows, V))
+    kind = (np.arange(rows) if rows > 1 else np.array([1])) % 6
+    for r in range(rows):
+        if kind[r] == 1:
+            at = int(rng.integers(0, V - 300))
+            z[r, at:at + 300] += 9
+        elif kind[r] == 2:
+            z[r, -200:] += 9
+        elif kind[r] == 3:
+            z[r] = np.round(z[r])
+        elif kind[r] == 4:
+            z[r, rng.random(V) < 0.999] -= 300
+        elif kind[r] == 5:
+            z[r] = 0.5
+    z = torch.from_numpy(z).to("cuda", DT[dt])
+    u = np.float32(rng.random(rows) * 0.99999)
+    t, p = np.float32(rng.uniform(0.5, 1.5, rows)), np.float32(rng.choice([0.3, 0.9, 1.0], rows))
+    for k in (1, 2, 24, 25, 96, 97, 192, 193):
+        check(z, u, call(z, u, t, [k] * rows), t, [k] * rows)
+        check(z, u, call(z, u, t, [k] * rows, p, np.float32([0.02] * rows)), t, [k] * rows, p, np.float32([0.02] * rows))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("V", [100, 20011])
 def test_ties_go_to_the_lower_index(V):
     """Few distinct values: the cut of top-k and top-p lies among equal logits, which the lower indexes survive."""
