@@ -14,7 +14,7 @@
 //   4  exact mass, tokens of the bins where top-p may cut                      rows with top-p
 //   5  exact mass of what stays, by index                                      all rows of many kept tokens
 // 256 rows of 50,001 16-bit logits with k = 50 take 27 us (41 by way of the histogram), 64 rows of 128,256 with settings of their own 69 us, one row of
-// 49,152 with top-p 22 us, 8 rows without filters 9 us.  Measured and left out: 1024 threads a CTA (+5 to +100 %), logits left in the L2 instead of shared
+// 49,152 with top-p 22 us, 8 rows without filters 8 us.  Measured and left out: 1024 threads a CTA (+5 to +100 %), logits left in the L2 instead of shared
 // memory (+10 to +20 % a pass), sorting up to 512 candidates instead of comparing up to 256 with each other (+30 %).
 #pragma once
 #include <cooperative_groups.h>
@@ -644,62 +644,81 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   }
 
   // ---- the draw: every warp has a run of neighbouring quads, its lanes take them in turn ----
-  const int lane = tid & 31, run = ((n_quad + THREADS - 1) / THREADS) * 32, r_lo = min(n_quad, (tid >> 5) * run), r_hi = min(n_quad, r_lo + run);
-  const unsigned key_cut = ~(unsigned)(cut >> MAX_VOCAB_BITS);  // (of no cut: 0)
-  const bool every = cut == ~0ull && least == 0.0;
-  auto few_of = [&](int i) -> u64 {  // mostly few stay: those that rank ahead of the cut, and only then their weights
-    const float4 q = quad_of(z_sm, i);
-    if (max(max(key_of(q.x), key_of(q.y)), max(key_of(q.z), key_of(q.w))) < key_cut) return 0;
-    const float z[4] = {q.x, q.y, q.z, q.w};
-    u64 sum = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const double w = weigh.scaled(z[j]);
-      sum += w >= least && place_of(z[j], v_first + i * 4 + j) <= cut ? Weigher::rounded(w) : 0;
-    }
-    return sum;
-  };
+  const int lane = tid & 31, warp = tid >> 5, run = ((n_quad + THREADS - 1) / THREADS) * 32, r_lo = min(n_quad, warp * run), r_hi = min(n_quad, r_lo + run);
   u64 mine = 0, total;
-  if (every) {
+  if (cut == ~0ull && least == 0.0) {
 #pragma unroll 2
     for (int i = r_lo + lane; i < r_hi; i += 32) {
       const float4 q = quad_of(z_sm, i);
       mine += (weigh(q.x) + weigh(q.y)) + (weigh(q.z) + weigh(q.w));
     }
   } else {
+    // Mostly few stay: those that rank ahead of the cut and are not far below what min-p asks for are put in a row, and weighed 32 at a time
+    const float low = least > 0.0 && top < INFINITY ? top + temp * (1.001f * __logf(fminf(min_p, 1.f)) - 1e-5f) - 1e-6f * fabsf(top) : -INFINITY;
+    const unsigned key_lo = max(~(unsigned)(cut >> MAX_VOCAB_BITS), low > -INFINITY ? key_of(low) : 0u);  // (of no cut: 0)
+    unsigned* line = reinterpret_cast<unsigned*>(smp_smem + p.hist_off) + warp * 160;
+    int in_line = 0;
+    auto worth = [&](unsigned e) -> u64 {
+      const double w = weigh_one(weigh, to_f32<T>(z_sm[e]));
+      return w >= least ? Weigher::rounded(w) : 0;
+    };
 #pragma unroll 1
-    for (int i = r_lo + lane; i < r_hi; i += 32) mine += few_of(i);
+    for (int i0 = r_lo; i0 < r_hi; i0 += 32) {
+      const int i = i0 + lane;
+      const float4 q = quad_of(z_sm, min(i, r_hi - 1));
+      const float z[4] = {q.x, q.y, q.z, q.w};
+      unsigned stays[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) stays[j] = __ballot_sync(0xffffffffu, i < r_hi && key_of(z[j]) >= key_lo && place_of(z[j], v_first + i * 4 + j) <= cut);
+      if ((stays[0] | stays[1] | stays[2] | stays[3]) == 0) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (stays[j] >> lane & 1) line[in_line + __popc(stays[j] & ((1u << lane) - 1))] = i * 4 + j;
+        in_line += __popc(stays[j]);
+      }
+      __syncwarp();
+#pragma unroll 1
+      for (; in_line >= 32; in_line -= 32) mine += worth(line[in_line - 32 + lane]);
+      __syncwarp();
+    }
+    if (lane < in_line) mine += worth(line[lane]);
   }
   u64 before = R.scan(mine, total);
   const u64 at = u > 0.f ? (u < 1.f ? times<false>(u, total) : total - 1) : 0;  // (total is 2^S at least: the largest logit stays)
+  // ... is in one warp's run, which all of its CTA go over again
+  if (tid == 0) s_found[0] = -1;
   const u64 end = __shfl_sync(0xffffffffu, before + mine, 31);
-  before = __shfl_sync(0xffffffffu, before, 0);
-  if (before <= at && at < end) {  // in this warp's run
+  __syncthreads();
+  if (lane == 0 && before <= at && at < end) s_found[0] = warp, s_before[0] = before;
+  __syncthreads();
+  if (s_found[0] < 0) return;
+  const int per = (run + THREADS - 1) / THREADS, f_lo = s_found[0] * run, f_hi = min(n_quad, f_lo + run);
+  const int e_lo = min(f_hi, f_lo + tid * per) * 4, e_hi = min(f_hi, f_lo + (tid + 1) * per) * 4;
+  mine = 0;
 #pragma unroll 1
-    for (int i = r_lo + lane; i - lane < r_hi; i += 32) {
-      const u64 x = i < r_hi ? few_of(i) : 0;
-      u64 upto = before + x;  // ... and the lanes' before this one
+  for (int i = e_lo / 4; i < e_hi / 4; ++i) {
+    const float4 q = quad_of(z_sm, i);
+    const float z[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 t = __shfl_up_sync(0xffffffffu, upto - before, o);
-        if (lane >= o) upto += t;
-      }
-      if (upto - x <= at && at < upto) {
-        u64 sum = upto - x;
+    for (int j = 0; j < 4; ++j) {
+      const double w = weigh.scaled(z[j]);
+      mine += w >= least && place_of(z[j], v_first + i * 4 + j) <= cut ? Weigher::rounded(w) : 0;
+    }
+  }
+  u64 sum;
+  before = s_before[0];
+  before += R.scan_block(mine, sum);
+  if (before <= at && at < before + mine) {
 #pragma unroll 1
-        for (int e = i * 4; e < i * 4 + 4; ++e) {
-          const float z = to_f32<T>(z_sm[e]);
-          const double w = weigh_one(weigh, z);
-          if (w < least || place_of(z, v_first + e) > cut) continue;
-          sum += Weigher::rounded(w);
-          if (sum > at) {
-            put(v_first + e, (float)(w / (double)total));
-            break;
-          }
-        }
+    for (int e = e_lo; e < e_hi; ++e) {
+      const float z = to_f32<T>(z_sm[e]);
+      const double w = weigh_one(weigh, z);
+      if (w < least || place_of(z, v_first + e) > cut) continue;
+      before += Weigher::rounded(w);
+      if (before > at) {
+        put(v_first + e, (float)(w / (double)total));
+        break;
       }
-      before = __shfl_sync(0xffffffffu, upto, 31);
-      if (before > at) break;
     }
   }
 }
