@@ -29,7 +29,6 @@ struct AppendParams {
   long long table_ld;    // elements from a row of the table to the next
   int table_w;
   int T, B, nq, rot;
-  int row_warps;          // warps of a CTA that share a row's heads: all of them, or 1
   int* err;
 };
 
@@ -51,17 +50,50 @@ struct AppRaw<float> {
   __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w; }
 };
 
+// Where a row's keys and values go, and its angles: a chain of four reads, one sine and cosine per pair of this lane
+struct AppRow {
+  bool in, ok;      // belongs to a sequence; its page is one of the cache
+  long long at;     // elements from the cache's start to the row's slot
+  float cs[4], sn[4];
+};
+__device__ __forceinline__ AppRow app_row(const AppendParams& p, int row, int lane, bool turns, int i0) {
+  AppRow r;
+  const int seq = seq_of_row(p.cu_rows, p.B, row, lane);
+  r.in = seq >= 0 && row < __ldg(p.cu_rows + max(seq, 0) + 1);
+  if (!r.in) return r;
+  const long long pos = (long long)__ldg(p.cached + seq) + (row - __ldg(p.cu_rows + seq));
+  const long long pg = pos >> p.kv.page_shift;
+  int page = -1;
+  if (pos >= 0 && pg < p.table_w) page = __ldg(p.page_table + seq * p.table_ld + pg);
+  r.ok = page >= 0 && page < p.kv.n_pages;
+  if (!r.ok && p.err && lane == 0) atomicOr(p.err, OP_BAD_PAGE);
+  const long long slot = pos & ((1ll << p.kv.page_shift) - 1);
+  r.at = (long long)page * p.kv.page_stride + slot * p.kv.slot_stride;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.cs[i] = 1.f, r.sn[i] = 0.f;
+  if (turns) {
+    const double index = (double)(pos + (p.pos_offset ? __ldg(p.pos_offset + seq) : 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      double t = index * __ldg(p.inv_freq + i0 + i) * 0.15915494309189533577;  // 1 / (2 pi): turns
+      t -= rint(t);
+      sincospif(2.f * (float)t, &r.sn[i], &r.cs[i]);
+    }
+  }
+  return r;
+}
+
+// Few rows: a row's heads over the warps of one CTA or several, for what counts is the way to the last store.
 // LH: lanes per head (a power of two >= d / 8)
 template <typename TI, typename TO, int LH>
 __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_constant__ AppendParams p) {
   constexpr int HPW = 32 / LH;                  // heads a warp works on at once
   constexpr int AHEAD = sizeof(TI) == 4 ? 2 : 3;  // such turns in flight: the look-ups below are a chain of four reads, and a row is over after a few turns
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row = p.row_warps == 1 ? blockIdx.x * APP_WARPS + warp : blockIdx.x, part = p.row_warps == 1 ? 0 : warp;
-  if (row >= p.T) return;
+  const int row = blockIdx.x;
   const int d = p.kv.d, n_heads = p.nq + 2 * p.kv.n_kv;
-  const int c = lane & (LH - 1), step = gridDim.y * p.row_warps * HPW;
-  const int h_warp = (blockIdx.y * p.row_warps + part) * HPW, h_lane = lane / LH;
+  const int c = lane & (LH - 1), step = gridDim.y * APP_WARPS * HPW;
+  const int h_warp = (blockIdx.y * APP_WARPS + warp) * HPW, h_lane = lane / LH;
   const bool live = c < d / 8, turns = 8 * c < p.rot;
   // this lane's elements: i0 .. i0 + 3 and i1 .. i1 + 3 of a head
   const int c0 = turns ? 4 * c : p.rot + 4 * (c - p.rot / 8), i0 = live ? c0 : 0, i1 = live ? i0 + (turns ? p.rot : d - p.rot) / 2 : 0;
@@ -76,27 +108,11 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
   };
   fetch(h_warp);
 
-  const int seq = seq_of_row(p.cu_rows, p.B, row, lane);
-  if (seq < 0 || row >= __ldg(p.cu_rows + seq + 1)) return;  // behind the last sequence: left as it was
-  const long long pos = (long long)__ldg(p.cached + seq) + (row - __ldg(p.cu_rows + seq));
-  const long long pg = pos >> p.kv.page_shift;
-  int page = -1;
-  if (pos >= 0 && pg < p.table_w) page = __ldg(p.page_table + seq * p.table_ld + pg);
-  const bool ok = page >= 0 && page < p.kv.n_pages;
-  if (!ok && p.err && lane == 0) atomicOr(p.err, OP_BAD_PAGE);
-  const long long slot = pos & ((1ll << p.kv.page_shift) - 1);
-  const long long at = (long long)page * p.kv.page_stride + slot * p.kv.slot_stride;
-
-  float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
-  if (live && turns) {
-    const double index = (double)(pos + (p.pos_offset ? __ldg(p.pos_offset + seq) : 0));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      double t = index * __ldg(p.inv_freq + i0 + i) * 0.15915494309189533577;  // 1 / (2 pi): turns
-      t -= rint(t);
-      sincospif(2.f * (float)t, &sn[i], &cs[i]);
-    }
-  }
+  const AppRow its = app_row(p, row, lane, live && turns, i0);
+  if (!its.in) return;  // behind the last sequence: left as it was
+  const bool ok = its.ok;
+  const long long at = its.at;
+  const float (&cs)[4] = its.cs, (&sn)[4] = its.sn;
   const float inv_d = 1.f / (float)d;
   // (the trip count is the warp's: its lanes shuffle together)
   for (int h0 = h_warp; h0 < n_heads; h0 += AHEAD * step) {
@@ -143,6 +159,105 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
       }
     }
   }
+}
+
+// Many rows: a warp per row, so that look-ups and sines are taken once for all heads.  Bound by the instructions per head as much as by the traffic (a loop
+// over all heads alike issued 170 a turn and took 48 us for 9,200 rows of 48 heads), so queries, keys and values have a loop each: values move as they
+// are, gains and addresses stay in registers, and the arithmetic is packed in pairs: 42 us, 4.6 TB/s, with norms or without - what is left is the
+// way of a row, four dependent look-ups ahead of its first store, in less than three rows per warp place.  More warps with fewer loads in flight each: +5 to +15 %.
+template <typename TI, typename TO, int LH>
+__global__ void __launch_bounds__(APP_WARPS * 32) append_rows_kernel(const __grid_constant__ AppendParams p) {
+  constexpr int HPW = 32 / LH, AHEAD = 4;
+  typedef unsigned long long u64;
+  const int lane = threadIdx.x & 31, row = blockIdx.x * APP_WARPS + (threadIdx.x >> 5);
+  if (row >= p.T) return;
+  const int d = p.kv.d, c = lane & (LH - 1), h_lane = lane / LH;
+  const bool live = c < d / 8, turns = 8 * c < p.rot;
+  const int c0 = turns ? 4 * c : p.rot + 4 * (c - p.rot / 8), i0 = live ? c0 : 0, i1 = live ? i0 + (turns ? p.rot : d - p.rot) / 2 : 0;
+  const TI* x = static_cast<const TI*>(p.qkv) + (long long)row * p.ld;
+  AppRaw<TI> ra[AHEAD], rb[AHEAD];
+  auto fetch = [&](const TI* from, int h0, int n) {
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) {
+      const int h = h0 + t * HPW + h_lane;
+      if (h < n) ra[t].load(from + h * d + i0), rb[t].load(from + h * d + i1);
+    }
+  };
+  fetch(x, 0, p.nq);
+  const AppRow its = app_row(p, row, lane, live && turns, i0);
+  if (!its.in) return;  // behind the last sequence: left as it was
+  const u64 cs[2] = {two(its.cs[0], its.cs[1]), two(its.cs[2], its.cs[3])}, sn[2] = {two(its.sn[0], its.sn[1]), two(its.sn[2], its.sn[3])};
+  const u64 ns[2] = {two(-its.sn[0], -its.sn[1]), two(-its.sn[2], -its.sn[3])};
+  const float inv_d = 1.f / (float)d;
+
+  // n heads from `from` (their first turns are on the way) to `to`, `stride` apart; then the first turns of the n_then heads at `then`
+  auto heads = [&](auto kind, const TI* from, int n, TO* to, long long stride, bool stored, const float* gain, const TI* then, int n_then) {
+    constexpr bool VALUES = decltype(kind)::value;
+    u64 g[4] = {0, 0, 0, 0};
+    if (!VALUES && gain) {
+      const float4 g0 = *reinterpret_cast<const float4*>(gain + i0), g1 = *reinterpret_cast<const float4*>(gain + i1);
+      g[0] = two(g0.x, g0.y), g[1] = two(g0.z, g0.w), g[2] = two(g1.x, g1.y), g[3] = two(g1.z, g1.w);
+    }
+#pragma unroll 1
+    for (int h0 = 0; h0 < n; h0 += AHEAD * HPW) {
+      AppRaw<TI> wa[AHEAD], wb[AHEAD];
+#pragma unroll
+      for (int t = 0; t < AHEAD; ++t) wa[t] = ra[t], wb[t] = rb[t];
+      if (h0 + AHEAD * HPW < n) fetch(from, h0 + AHEAD * HPW, n);
+      else fetch(then, 0, n_then);
+#pragma unroll
+      for (int t = 0; t < AHEAD; ++t) {
+        if (h0 + t * HPW >= n) break;
+        const int h = h0 + t * HPW + h_lane;
+        const bool here = live && h < n;
+        TO* dst = to + h * stride;
+        if constexpr (VALUES && std::is_same<TI, TO>::value) {
+          if (here && stored) *reinterpret_cast<uint2*>(dst + i0) = wa[t].w, *reinterpret_cast<uint2*>(dst + i1) = wb[t].w;
+          continue;
+        } else {
+          float f[8];
+          wa[t].get(reinterpret_cast<float(&)[4]>(f[0])), wb[t].get(reinterpret_cast<float(&)[4]>(f[4]));
+          u64 v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = two(f[2 * i], f[2 * i + 1]);
+          if (!VALUES) {
+            if (gain) {
+              u64 sq = mul2(v[0], v[0]);
+#pragma unroll
+              for (int i = 1; i < 4; ++i) sq = fma2(v[i], v[i], sq);
+              float s0, s1;
+              split(sq, s0, s1);
+              float ss = here ? s0 + s1 : 0.f;
+#pragma unroll
+              for (int o = LH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+              const float r = rsqrtf(ss * inv_d + p.eps);  // (2 ulp)
+              const u64 r2 = two(r, r);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], mul2(r2, g[i]));
+            }
+            if (turns) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const u64 a = v[i], b = v[2 + i];
+                v[i] = fma2(b, ns[i], mul2(a, cs[i])), v[2 + i] = fma2(a, sn[i], mul2(b, cs[i]));
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
+          if (here && stored) {
+            *reinterpret_cast<uint2*>(dst + i0) = make_uint2(pack2<TO>(f[0], f[1]), pack2<TO>(f[2], f[3]));
+            *reinterpret_cast<uint2*>(dst + i1) = make_uint2(pack2<TO>(f[4], f[5]), pack2<TO>(f[6], f[7]));
+          }
+        }
+      }
+    }
+  };
+  const TI *xk = x + (long long)p.nq * d, *xv = xk + (long long)p.kv.n_kv * d;
+  if (p.nq == 0) fetch(xk, 0, p.kv.n_kv);
+  heads(std::false_type(), x, p.nq, static_cast<TO*>(p.q) + (long long)row * p.q_ld, d, true, p.q_norm, xk, p.kv.n_kv);
+  heads(std::false_type(), xk, p.kv.n_kv, static_cast<TO*>(p.kv.k) + its.at, p.kv.head_stride, its.ok, p.k_norm, xv, p.kv.n_kv);
+  heads(std::true_type(), xv, p.kv.n_kv, static_cast<TO*>(p.kv.v) + its.at, p.kv.head_stride, its.ok, nullptr, xv, 0);
 }
 
 }  // namespace ls

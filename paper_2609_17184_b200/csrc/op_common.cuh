@@ -46,6 +46,29 @@ __device__ __forceinline__ unsigned pack2<__half>(float a, float b) {
   return *reinterpret_cast<const unsigned*>(&v);
 }
 
+// Blackwell's packed fp32 arithmetic: two values a register pair
+__device__ __forceinline__ unsigned long long two(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(unsigned long long x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // The sequence that token row `row` belongs to: the last b < B with cu[b] <= row (-1: none).  A whole warp asks; every round probes 32
 // places, so the dependent loads are two up to 1024 sequences.  Whatever cu holds, the answer lies in [-1, B).
 __device__ __forceinline__ int seq_of_row(const int* cu, int B, int row, int lane) {

@@ -38,23 +38,6 @@ __device__ __forceinline__ void pxt_ld16(unsigned (&v)[16], unsigned taddr) {
                : "r"(taddr)
                : "memory");
 }
-// Blackwell's packed fp32 arithmetic: two values a register pair
-__device__ __forceinline__ unsigned long long pxt_two(float a, float b) {
-  unsigned long long r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void pxt_split(unsigned long long x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
-__device__ __forceinline__ unsigned long long pxt_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-  unsigned long long r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ unsigned long long pxt_add2(unsigned long long a, unsigned long long b) {
-  unsigned long long r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ float pxt_max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -314,7 +297,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
       if (__any_sync(0xffffffffu, to != ref)) l *= to == ref || j == 0 ? 1.f : px_exp2(ref - to);
       ref = to;
       const float sub = ref == -INFINITY ? 0.f : ref;
-      const unsigned long long sc2 = pxt_two(p.scale_log2, p.scale_log2), sub2 = pxt_two(-sub, -sub);
+      const unsigned long long sc2 = two(p.scale_log2, p.scale_log2), sub2 = two(-sub, -sub);
       if (j > 0) px_wait(&sh.pv[st], (done + j - 1) & 1, ok);  // this stream's last weights are used up
       unsigned long long sum[2] = {0, 0};
 #pragma unroll
@@ -323,9 +306,9 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float a, b;
-          pxt_split(pxt_fma2(pxt_two(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), sc2, sub2), a, b);
+          split(fma2(two(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), sc2, sub2), a, b);
           a = px_exp2(a), b = px_exp2(b);
-          sum[e & 1] = pxt_add2(sum[e & 1], pxt_two(a, b));
+          sum[e & 1] = add2(sum[e & 1], two(a, b));
           wt[e] = pack2<T>(a, b);
         }
         pxt_st16(t_p + 16 * c, wt);
@@ -336,7 +319,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
         }
       }
       float a, b;
-      pxt_split(pxt_add2(sum[0], sum[1]), a, b);
+      split(add2(sum[0], sum[1]), a, b);
       l += a + b;
     }
     // ---- the row's partial: warps 0 .. 3 the first half of its elements, 4 .. 7 the second ----

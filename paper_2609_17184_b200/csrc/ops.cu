@@ -55,22 +55,26 @@ bool paged_kv(const loopspec_paged_kv* c, PagedKv* o) {
 
 using AppendFn = void (*)(const AppendParams);
 template <typename TI, typename TO>
-AppendFn append_fn(int lh) {
+AppendFn append_fn(int lh, bool rows) {
   switch (lh) {
-    case 1: return append_kernel<TI, TO, 1>;
-    case 2: return append_kernel<TI, TO, 2>;
-    case 4: return append_kernel<TI, TO, 4>;
-    case 8: return append_kernel<TI, TO, 8>;
-    case 16: return append_kernel<TI, TO, 16>;
-    default: return append_kernel<TI, TO, 32>;
+    case 1: return rows ? append_rows_kernel<TI, TO, 1> : append_kernel<TI, TO, 1>;
+    case 2: return rows ? append_rows_kernel<TI, TO, 2> : append_kernel<TI, TO, 2>;
+    case 4: return rows ? append_rows_kernel<TI, TO, 4> : append_kernel<TI, TO, 4>;
+    case 8: return rows ? append_rows_kernel<TI, TO, 8> : append_kernel<TI, TO, 8>;
+    case 16: return rows ? append_rows_kernel<TI, TO, 16> : append_kernel<TI, TO, 16>;
+    default: return rows ? append_rows_kernel<TI, TO, 32> : append_kernel<TI, TO, 32>;
   }
 }
 template <typename TO>
-AppendFn append_fn(int dtype, int lh) {
-  return dtype == 0 ? append_fn<float, TO>(lh) : dtype == 1 ? append_fn<__nv_bfloat16, TO>(lh) : append_fn<__half, TO>(lh);
+AppendFn append_fn(int dtype, int lh, bool rows) {
+  return dtype == 0 ? append_fn<float, TO>(lh, rows) : dtype == 1 ? append_fn<__nv_bfloat16, TO>(lh, rows) : append_fn<__half, TO>(lh, rows);
 }
 
 constexpr int kSms = 148;
+// Token rows from which append_kv gives each a warp of its own; below, a row's heads are spread over warps [us spread / a warp each: 48 heads of 128 with
+// norms 300 rows 5.9 / 7.9, 600 6.9 / 8.8, 1000 10.0 / 9.2, 1990 15.4 / 11.8, 8000 50 / 36; 48 heads of 64 without 300 5.0 / 4.3, 600 4.6 / 4.9, 1000
+// 6.4 / 5.1, 1990 9.0 / 6.1]
+constexpr int APP_ROWS = 1000;
 
 // Lets a kernel ask for `bytes` of dynamic shared memory; `done` remembers, a bit per device, that it may.  regs: registers a thread that it must have
 // been compiled to (0: any)
@@ -215,14 +219,11 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
   p.T = T, p.B = n_seqs, p.nq = n_q_heads, p.rot = rot_dim, p.err = flag;
   int lh = 1;
   while (lh < p.kv.d / 8) lh *= 2;
-  const AppendFn fn = kv->dtype == 1 ? append_fn<__nv_bfloat16>(qkv_dtype, lh) : append_fn<__half>(qkv_dtype, lh);
-  // Few rows: a row's heads over the warps of several CTAs, for what counts is the way to the last store.  Many: a warp per row, so that look-ups and sines
-  // are taken once for all heads [us with all warps / with one, 48 heads of 128 with norms: 8000 rows 50 / 44, 2000 14.8 / 15.1, 1000 9.5 / 12.2, 200 5.4 /
-  // 11; 48 heads of 64 without: 8000 29 / 19, 2000 8.9 / 7.2, 1000 6.0 / 5.9].
-  p.row_warps = T >= 2000 ? 1 : APP_WARPS;
-  const int per_turn = p.row_warps * (32 / lh), turns = (int)((n_q_heads + 2 * (int64_t)p.kv.n_kv + per_turn - 1) / per_turn);
-  const int split = p.row_warps == 1 ? 1 : std::max(1, std::min(turns, 1184 / T));
-  return launch(fn, dim3(p.row_warps == 1 ? (T + APP_WARPS - 1) / APP_WARPS : T, split), APP_WARPS * 32, 0, cuda_stream, p);
+  const bool rows = T >= APP_ROWS;
+  const AppendFn fn = kv->dtype == 1 ? append_fn<__nv_bfloat16>(qkv_dtype, lh, rows) : append_fn<__half>(qkv_dtype, lh, rows);
+  if (rows) return launch(fn, dim3((T + APP_WARPS - 1) / APP_WARPS, 1), APP_WARPS * 32, 0, cuda_stream, p);
+  const int per_turn = APP_WARPS * (32 / lh), turns = (int)((n_q_heads + 2 * (int64_t)p.kv.n_kv + per_turn - 1) / per_turn);
+  return launch(fn, dim3(T, std::max(1, std::min(turns, 1184 / T))), APP_WARPS * 32, 0, cuda_stream, p);
 }
 
 size_t loopspec_prefix_attention_scratch_bytes(int32_t T, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t prefix_len) {

@@ -88,6 +88,11 @@ CASES = [
     ([2, 1] * 700, [0, 1] * 700, 2, 1, 16, 2, "fp32", "bf16", 16, False, 7, None),
     ([1100, 0, 1299], [5, 7, 0], 3, 2, 64, 32, "bf16", "bf16", 32, True, 3, None),  # a warp per row
     ([2050], [1], 2, 1, 40, 16, "fp32", "fp16", 40, False, 1, [3]),
+    ([1000], [0], 0, 3, 8, 1, "bf16", "bf16", 8, True, 5, None),
+    ([700, 0, 401], [3, 2, 9], 9, 3, 128, 16, "fp16", "fp16", 128, True, 2, [9, 0, 1000003]),
+    ([1001], [2], 7, 1, 256, 64, "fp32", "bf16", 256, True, 0, None),
+    ([1, 998, 1], [0, 5, 0], 17, 5, 96, 8, "fp32", "fp16", 0, True, 0, None),
+    ([1000], [7], 1, 1, 64, 32, "bf16", "bf16", 24, False, 0, None),
 ]
 
 
@@ -176,6 +181,32 @@ def test_bad_entries_leave_a_flag_and_nothing_else():
         call(g, flag=flag)
         assert flag.item() == 1
         call(g)  # (no flag asked for)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gains", [(True, False), (False, True)])
+def test_a_prompt_with_bad_pages_one_gain_and_numbers_that_are_none(gains):
+    s, g = make([600, 500], [1, 4], 6, 2, 64, 16, "bf16", "bf16", 64, True, pad=3)
+    for key, keep in zip(("qn", "kn"), gains):
+        if not keep:
+            s[key] = g[key] = None
+    bad = (0, 3)  # positions 48 .. 63 of the first sequence: rows 47 .. 62
+    s["table"] = s["table"].clone()
+    g["table"][bad] = g["kv"].size(0)
+    g["x"][700] = float("nan")
+    g["x"][-3:] = float("inf")  # (padding)
+    before = g["kv"].clone()
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    call(g, flag=flag)
+    assert flag.item() == 1
+    lost = int(s["table"][bad])
+    assert torch.equal(g["kv"][lost], before[lost])
+    at = int(s["table"][1, 104 // 16]), 104 % 16  # row 700: position 104 of the second sequence
+    assert g["q"][700].isnan().all() and g["kv"][at[0], :, :, at[1]].isnan().all()
+    q, kv, tq, tkv = reference(s)
+    dq, dkv = (g["q"].double().cpu() - q).abs() <= tq, (g["kv"].double().cpu() - kv).abs() <= tkv
+    dq[700], dkv[lost], dkv[at[0], :, :, at[1]] = True, True, True
+    assert dq.all() and dkv.all()
 
 
 @pytest.mark.gpu
