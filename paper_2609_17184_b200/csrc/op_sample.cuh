@@ -34,6 +34,8 @@ constexpr int LIST = 2048;         // tokens one CTA can be sent, an equal part 
 constexpr int SOLO = 256;          // candidates with which one CTA finishes a row alone
 static_assert(2 * SOLO == THREADS, "the list's companion holds a pair for each of them, or a sum for each thread");
 constexpr int QUICK = 192;         // top-k times CTAs of a row up to which that is tried without a histogram (some half as many tokens more are sent)
+constexpr int LINE = 160;          // tokens a warp has room for: 31 that wait and four a lane
+static_assert(WARPS * LINE * 4 <= (LIST + 2 * SOLO) * 8, "in the list's place");
 constexpr int MAX_VOCAB_BITS = 18;
 
 struct Params {
@@ -656,7 +658,8 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
     // Mostly few stay: those that rank ahead of the cut and are not far below what min-p asks for are put in a row, and weighed 32 at a time
     const float low = least > 0.0 && top < INFINITY ? top + temp * (1.001f * __logf(fminf(min_p, 1.f)) - 1e-5f) - 1e-6f * fabsf(top) : -INFINITY;
     const unsigned key_lo = max(~(unsigned)(cut >> MAX_VOCAB_BITS), low > -INFINITY ? key_of(low) : 0u);  // (of no cut: 0)
-    unsigned* line = reinterpret_cast<unsigned*>(smp_smem + p.hist_off) + warp * 160;
+    // (in the list's place: the histogram ahead of it may still be read by the cluster's other CTAs, where no cut was looked for in the list)
+    unsigned* line = reinterpret_cast<unsigned*>(smp_smem + p.hist_off + BINS * 8) + warp * LINE;
     int in_line = 0;
     auto worth = [&](unsigned e) -> u64 {
       const double w = weigh_one(weigh, to_f32<T>(z_sm[e]));

@@ -103,6 +103,22 @@ def test_cuts_that_leave_thousands_of_tokens(V, dt, spread):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V,dt", [(128256, "fp32"), (50001, "bf16")])
+def test_a_top_k_of_more_tokens_than_weigh_anything_with_min_p(V, dt):
+    """Low temperatures: thousands of tokens weigh something, fewer than top-k would keep, and min-p has the last word; again and again, in clusters of
+    every size."""
+    rng = np.random.default_rng(V)
+    for rows in (1, 3, 30, 80):
+        z = torch.from_numpy(rng.standard_normal((rows, V))).to("cuda", DT[dt])
+        u, t, k = np.float32(rng.random(rows) * 0.99999), np.float32([0.08] * rows), [V - 1] * rows
+        for m in (np.float32([0.01] * rows), np.float32([1e-9] * rows), np.float32([1.0] * rows)):
+            first = [x.clone() for x in call(z, u, t, k, None, m)]
+            check(z, u, first, t, k, None, m)
+            for _ in range(10):
+                assert all(torch.equal(a, b) for a, b in zip(call(z, u, t, k, None, m), first))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,V,dt", [(1, 50001, "fp32"), (20, 20011, "bf16"), (40, 9000, "fp16"), (160, 5003, "fp32"), (300, 700, "bf16")])
 def test_a_small_k_wherever_its_tokens_lie(rows, V, dt):
     """The largest logits spread, side by side, at either end, many alike, or fewer that weigh anything than k."""
