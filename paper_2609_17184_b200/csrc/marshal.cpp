@@ -72,10 +72,15 @@ loopspec_paged_kv paged(PyObject* ko, PyObject* vo, at::Device dev) {
   const at::ScalarType type = k.scalar_type();
   if ((type != at::kBFloat16 && type != at::kHalf) || v.scalar_type() != type || k.dim() != 4 || v.dim() != 4 || !on(k, dev) || !on(v, dev))
     refuse("k_cache, v_cache: [pages, heads, page_size, head_dim] bf16 or fp16 on " + dev.str() + " are needed");
-  if (v.sizes() != k.sizes() || v.strides() != k.strides() || (k.stride(3) != 1 && k.size(3) > 1))
-    refuse("k_cache, v_cache: one shape and one set of strides are needed, the last dimension contiguous");
+  bool alike = v.sizes() == k.sizes() && (k.stride(3) == 1 || k.size(3) <= 1);
+  int64_t stride[3];  // (of a dimension of one element any stride will do)
+  for (int i = 0; alike && i < 3; ++i) {
+    stride[i] = k.size(i) > 1 ? k.stride(i) : k.size(3);
+    alike = k.size(i) <= 1 || v.stride(i) == stride[i];
+  }
+  if (!alike) refuse("k_cache, v_cache: one shape and one set of strides are needed, the last dimension contiguous");
   loopspec_paged_kv c;
-  c.k = k.data_ptr(), c.v = v.data_ptr(), c.page_stride = k.stride(0), c.head_stride = k.stride(1), c.slot_stride = k.stride(2);
+  c.k = k.data_ptr(), c.v = v.data_ptr(), c.page_stride = stride[0], c.head_stride = stride[1], c.slot_stride = stride[2];
   c.n_pages = int32_of(k.size(0), "k_cache"), c.n_kv_heads = int32_of(k.size(1), "k_cache"), c.page_size = int32_of(k.size(2), "k_cache");
   c.head_dim = int32_of(k.size(3), "k_cache"), c.dtype = code_of(type);
   return c;
@@ -86,7 +91,7 @@ int64_t heads(const at::Tensor& t, const char* what, at::ScalarType type, int64_
       (t.numel() && ((t.stride(2) != 1 && d > 1) || (t.stride(1) != d && n > 1))))
     refuse(std::string(what) + ": [" + std::to_string(rows) + ", " + std::to_string(n) + ", " + std::to_string(d) + "] " + c10::toString(type) + " on " + dev.str() +
            " with contiguous heads is needed");
-  return t.stride(0);
+  return rows > 1 ? t.stride(0) : n * d;
 }
 void done(int rc, const char* what) {
   if (rc) throw Refused{rc, what};
@@ -148,7 +153,7 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* flag = static_cast<int32_t*>(vec(a[13], "flag", at::kInt, 1, dev, true));
     const float eps = float_arg(a[10]);
     call(dev, "append_kv", [&](void* st) {
-      return loopspec_op_append_kv(qkv.data_ptr(), code, qkv.stride(0), T, nq, &kv, pt.ptr, pt.ld, pt.width, cached, cu, pt.rows, off, freq, int32_of(2 * half, "inv_freq"), qn, kn,
+      return loopspec_op_append_kv(qkv.data_ptr(), code, T > 1 ? qkv.stride(0) : qkv.size(1), T, nq, &kv, pt.ptr, pt.ld, pt.width, cached, cu, pt.rows, off, freq, int32_of(2 * half, "inv_freq"), qn, kn,
                                    eps, out.data_ptr(), q_ld, flag, st);
     });
     if (a[12] != Py_None) return Py_INCREF(a[12]), a[12];
@@ -181,6 +186,7 @@ PyObject* prefix_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* lens = static_cast<int32_t*>(vec(a[6], "lens", at::kInt, pt.rows, dev));
     const int32_t* cu = static_cast<int32_t*>(vec(a[7], "cu_rows", at::kInt, (int64_t)pt.rows + 1, dev));
     const float scale = a[8] == Py_None ? 0.f : float_arg(a[8]);
+    if (a[8] != Py_None && scale == 0.f) refuse("scale: a positive number is needed (None: 1 / sqrt(head_dim))");
     int32_t* flag = static_cast<int32_t*>(vec(a[12], "flag", at::kInt, 1, dev, true));
     const size_t need = loopspec_prefix_attention_scratch_bytes(T, pt.rows, nq, kv.n_kv_heads, kv.head_dim, P);
     if (need == 0) refuse("prefix_attention: head_dim 64 or 128, n_q_heads a multiple of the key heads, at most 2048 sequences");

@@ -227,6 +227,16 @@ def test_not_a_number_stays_in_its_row():
 
 
 @pytest.mark.gpu
+def test_dimensions_of_one_element_have_any_stride():
+    s, g = make([1], [5], 3, 1, 64, 1, "fp32", "bf16", 64, True)
+    for name in ("x", "q", "kv"):
+        x = g[name]
+        g[name] = x.as_strided(x.shape, [3 if n == 1 else st for n, st in zip(x.shape, x.stride())])
+    call(g)
+    check(s, g)
+
+
+@pytest.mark.gpu
 def test_no_rows_and_padding_only():
     s, g = make([2], [0], 2, 1, 64, 16, "bf16", "bf16", 64, False)
     kv, q = g["kv"].clone(), g["q"].clone()

@@ -119,6 +119,14 @@ def test_against_64_bits(i):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,own", [(64, True), (128, False)])
+def test_more_row_tiles_than_sms(d, own):
+    """1200 rows of 16 query heads to a key head: 150 tiles of 128 rows for the prefix, two rounds of them."""
+    s = make(270, [300] * 4, [310, 300, 305, 320] if own else [0] * 4, 32, 2, d, 16, "bf16", seed=11)
+    check(s, *call(s), rows={0, 5, 299, 300, 599, 777, 1199})
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("d", [64, 128])
 def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(d, bad):
@@ -246,6 +254,15 @@ def test_flags():
 
 
 @pytest.mark.gpu
+def test_dimensions_of_one_element_have_any_stride():
+    s = make(13, [1], [9], 3, 1, 64, 1, "bf16", seed=12)
+    for name in ("q", "kv"):
+        x = s[name]
+        s[name] = x.as_strided(x.shape, [3 if n == 1 else st for n, st in zip(x.shape, x.stride())])
+    check(s, *call(s))
+
+
+@pytest.mark.gpu
 def test_nothing_to_do():
     s = make(10, [1], [3], 2, 1, 64, 16, "bf16")
     s["q"] = s["q"][:0]
@@ -304,4 +321,6 @@ def test_wrapper_refusals():
     fails(cu=lambda x: x[:2])
     fails(call_kw=dict(out=torch.zeros(2, 4, 64, dtype=torch.bfloat16, device="cuda")))
     fails(call_kw=dict(lse=torch.zeros(3, 3, device="cuda")))
+    fails(call_kw=dict(scale=0.0))
+    fails(call_kw=dict(scale=-1.0))
     fails("ECAPACITY", call_kw=dict(scratch=torch.zeros(256, dtype=torch.uint8, device="cuda")))
