@@ -314,8 +314,8 @@ typedef struct {
  * rotated: pairs (i, i + rot_dim / 2) of the first rot_dim elements turn by index * inv_freq[i] (fp64 [rot_dim / 2], radians per position;
  * rot_dim % 8 == 0, 0 = no rotation), index = position + pos_offset[b] (int32 [n_seqs], NULL = 0: the length of a shared prefix, say).  The angle is taken
  * in 64 bits, the rest in fp32 and rounded once to the cache's type; q_out: [T] rows of n_q_heads heads of that type, q_ld elements apart
- * (n_q_heads = 0: keys and values only).  qkv and q_out: 16-byte aligned, rows multiples of 8 elements.  Row 0 of every sequence may be any number of
- * positions; two sequences must not own the same page at the positions being written.  flag: int32 that the call ors its bits into, or NULL. */
+ * (n_q_heads = 0: keys and values only).  qkv and q_out: 16-byte aligned, rows multiples of 8 elements.  Two sequences must not
+ * own the same page at the positions being written.  flag: int32 that the call ors its bits into, or NULL. */
 int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv,
                           const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* cached, const int32_t* cu_rows, int32_t n_seqs,
                           const int32_t* pos_offset, const double* inv_freq, int32_t rot_dim, const float* q_norm, const float* k_norm, float eps,
@@ -324,7 +324,7 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
 /* Attention of T new rows of n_seqs sequences that share a prefix: row j (of n) of sequence b, one of cu_rows[b] .. cu_rows[b + 1] - 1, attends to the
  * prefix - prefix_len positions in the pages prefix_pages (int32 [ceil(prefix_len / page_size)]) - and to the sequence's own positions
  * below lens[b] - (n - 1 - j) of page_table[b] (own position 0 in its first page; lens[b] counts the new rows, appended beforehand, so the
- * last row sees all of them).  out = softmax(scale * q K^T) V per query head, heads n_q_heads / n_kv_heads to a key head; scale 0 = 1 / sqrt(head_dim).
+ * last row sees all of them).  out = softmax(scale * q K^T) V per query head, heads n_q_heads / n_kv_heads to a key head; scale: positive, 0 = 1 / sqrt(head_dim).
  * The prefix's keys and values are read and multiplied once for all sequences.  A row that sees no key gets zeros (lse -inf).  Keys and values behind
  * what a row sees do not enter it, whatever they hold.  q, out: [T] rows of n_q_heads heads of the cache's type, q_ld / out_ld
  * elements apart, 16-byte aligned, multiples of 8 elements; lse: fp32 [T][n_q_heads], the natural logarithm of the sum of the exponentials, or NULL.  Rows from cu_rows[n_seqs]
