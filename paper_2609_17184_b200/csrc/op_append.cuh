@@ -37,6 +37,7 @@ template <typename T>
 struct AppRaw {
   uint2 w;
   __device__ __forceinline__ void load(const T* p) { w = __ldcs(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void store(void* p) const { *static_cast<uint2*>(p) = w; }
   __device__ __forceinline__ void get(float (&v)[4]) const {
     const T* e = reinterpret_cast<const T*>(&w);
 #pragma unroll
@@ -47,6 +48,7 @@ template <>
 struct AppRaw<float> {
   float4 w;
   __device__ __forceinline__ void load(const float* p) { w = __ldcs(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void store(void* p) const { *static_cast<float4*>(p) = w; }
   __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w; }
 };
 
@@ -211,8 +213,8 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_rows_kernel(const __gri
         const int h = h0 + t * HPW + h_lane;
         const bool here = live && h < n;
         TO* dst = to + h * stride;
-        if constexpr (VALUES && std::is_same<TI, TO>::value) {
-          if (here && stored) *reinterpret_cast<uint2*>(dst + i0) = wa[t].w, *reinterpret_cast<uint2*>(dst + i1) = wb[t].w;
+        if constexpr (VALUES && std::is_same<TI, TO>::value) {  // as they are
+          if (here && stored) wa[t].store(dst + i0), wb[t].store(dst + i1);
           continue;
         } else {
           float f[8];
