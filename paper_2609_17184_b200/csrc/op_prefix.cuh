@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(PX_THREADS, 1)
 // instruction cache (16 KB of it took 10 us where there were 35 partials to fold).
 template <typename T, int D, int WPR>
 __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant__ PrefixParams p) {
-  constexpr int V = D / 32, AHEAD = 4;  // elements per lane, partials in flight
+  constexpr int V = D / 32, AHEAD = WPR > 1 ? 12 : 4;  // elements per lane, partials in flight
   __shared__ float s_o[WPR > 1 ? 4 : 1][D], s_ml[4][2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = WPR > 1 ? blockIdx.x : blockIdx.x * 4 + warp;
   const int b = at / p.nq, head = at - b * p.nq, h = head / p.G;
@@ -90,9 +90,10 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
 #pragma unroll 1
-    for (int x0 = WPR > 1 ? warp * 32 : 0; x0 < count; x0 += 32 * WPR) {
+    for (int x0 = WPR > 1 ? warp : 0; x0 < count; x0 += 32 * WPR) {  // (the warps take them in turn)
       // this lane's partial: the first of a tile is in the tile's own slot, the others in those of the workers that follow
-      int x = x0 + lane;
+      int x = x0 + lane * WPR;
+      const int cnt = min(32, (count - x0 + WPR - 1) / WPR);
       const float *po = p.item_o, *pm = p.item_ml;
       long long slot = 0;
       if (x < st.y) {
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
         if (x) po = p.warp_o, pm = p.warp_ml;
       }
       float2 ml = make_float2(-INFINITY, 0.f);
-      if (x0 + lane < count) ml = __ldcg(reinterpret_cast<const float2*>(pm) + slot);
+      if (lane < cnt) ml = __ldcg(reinterpret_cast<const float2*>(pm) + slot);
       unsigned long long src = reinterpret_cast<unsigned long long>(po + slot * D);
       const float mx = fmaxf(m, warp_max(ml.x)), ref = mx == -INFINITY ? 0.f : mx;
       const float wt = px_exp2(ml.x - ref), keep = px_exp2(m - ref);
@@ -114,7 +115,6 @@ __global__ void __launch_bounds__(128) prefix_merge_kernel(const __grid_constant
       l = l * keep + warp_sum(ml.y * wt);
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[e] *= keep;
-      const int cnt = min(32, count - x0);
 #pragma unroll 1
       for (int y0 = 0; y0 < cnt; y0 += AHEAD) {
         float v[AHEAD][V], f[AHEAD];

@@ -171,10 +171,11 @@ int px_launch(PrefixParams& p, const PxPlan& t, int dtype, void* stream) {
     (void)cudaGetLastError();
     return LOOPSPEC_ECUDA;
   }
-  // the fold: a CTA per sequence and query head while there are few rows, else a warp; long runs of rows over several
+  // the fold: a CTA per sequence and query head while there are few rows, else a warp (16 rows x heads 9.0 / 10.6 us, 640 15.7 / 18.5, 2048 45.9 / 37.4);
+  // long runs of rows over several
   const int64_t heads = (int64_t)p.B * p.nq;
   const unsigned y = (unsigned)std::min<int64_t>(64, std::max<int64_t>(1, ((int64_t)p.T * 2 + p.B - 1) / p.B));
-  if ((int64_t)p.T * p.nq <= 4 * kSms) return launch(prefix_merge_kernel<T, D, 4>, dim3((unsigned)heads, y), 128, 0, stream, p, true);
+  if ((int64_t)p.T * p.nq <= 8 * kSms) return launch(prefix_merge_kernel<T, D, 4>, dim3((unsigned)heads, y), 128, 0, stream, p, true);
   return launch(prefix_merge_kernel<T, D, 1>, dim3((unsigned)((heads + 3) / 4), y), 128, 0, stream, p, true);
 }
 
