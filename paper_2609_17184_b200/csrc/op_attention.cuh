@@ -10,7 +10,7 @@
 //
 // The two kinds of work want different parts of the machine, so they run side by side: every CTA adds up from the lengths what there is of either
 // and takes the role that makes both end together.  (One after the other, 256 sequences of 16 heads behind 16384 positions took 122 us
-// where the stream alone takes 50 and the products 45.)
+// where the stream alone takes 57 and the prefix alone 62; side by side they take 102.)
 //
 // Scores are bf16 / fp16 products summed in fp32; maximum, sum and weighted values are fp32.  The softmax weights are rounded to the cache's
 // type for the second contraction: an error of half a step of the output's own type per weight, averaged over the keys.
