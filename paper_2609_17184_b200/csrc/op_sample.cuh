@@ -272,6 +272,8 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   const float temp = p.temperature ? __ldg(p.temperature + row) : 1.f, u = __ldg(p.u + row);
   const float top_p = p.top_p ? __ldg(p.top_p + row) : 1.f, min_p = p.min_p ? __ldg(p.min_p + row) : 0.f;
   const int top_k = p.top_k ? __ldg(p.top_k + row) : 0;
+  // Another CTA's shared memory is there only once that CTA has started: each says so here, and the slice's load covers the wait for the others
+  if (R.n > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
 
   // ---- the slice as it lies in memory, 16 bytes at a time; what of the first and the last 16 is not the slice's counts as masked out.  (A logit that is
   // no number is treated so wherever it is compared.) ----
@@ -299,6 +301,7 @@ __global__ void __launch_bounds__(THREADS, 2) sample_kernel(const __grid_constan
   }
   if (tid < 256) s_table[tid] = exp2((double)tid / 256);
   const float own_top = top;
+  if (R.n > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // (before the first word that goes to another CTA)
   const unsigned top_key = (unsigned)R.max(key_of(top));
   top = logit_of(top_key);
   auto put = [&](int token, float prob) {

@@ -1,5 +1,6 @@
 """sample: a token per row by temperature, top-k, top-p and min-p from given uniform numbers."""
 import math
+import pathlib
 
 import numpy as np
 import pytest
@@ -262,6 +263,28 @@ def test_offsets_beyond_32_bits():
     z.copy_(torch.randn(rows, V))
     u = np.float32([0.1, 0.5, 0.9])
     check(z, u, call(z, u, None, None, np.float32([0.9] * 3)), None, None, np.float32([0.9] * 3))
+
+
+def test_no_cta_reaches_into_another_before_all_of_its_cluster_have_started():
+    """Read off the source, for what it prevents is a fault: every CTA of a cluster arrives at its barrier, and waits there ahead of the first exchange (a
+    reduction, or an address in another CTA's shared memory)."""
+    body = (pathlib.Path(__file__).parents[1] / "paper_2609_17184_b200/csrc/op_sample.cuh").read_text().split("sample_kernel(const __grid_constant__ Params p)")[1]
+    arrive, wait = body.find("barrier.cluster.arrive"), body.find("barrier.cluster.wait")
+    assert 0 <= arrive < wait < min(body.find(x) for x in ("R.max(", "R.sum(", "R.scan(", "cl.sync(", "map_shared_rank("))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,V", [(1, 16384), (30, 2056), (3, 2049), (2, 262144)])
+def test_clusters_that_begin_again_and_again(rows, V):
+    """Slices of some 260 to 1000 tokens (and a long one), whose load leaves next to no time between a CTA's start and its first exchange."""
+    rng = np.random.default_rng(rows)
+    z = torch.from_numpy(rng.standard_normal((rows, V)).astype(np.float32)).cuda()
+    u, k = torch.from_numpy(rng.random(rows, dtype=np.float32) * 0.9999).cuda(), torch.full((rows,), 20, dtype=torch.int32, device="cuda")
+    plain, few = [x.clone() for x in ls.sample(z, u)], [x.clone() for x in ls.sample(z, u, top_k=k)]
+    check(z, u.cpu().numpy(), plain)
+    got = [(ls.sample(z, u), ls.sample(z, u, top_k=k)) for _ in range(200)]
+    for a, b in got:
+        assert all(torch.equal(x, y) for x, y in zip((*a, *b), (*plain, *few)))
 
 
 def test_refusals():
