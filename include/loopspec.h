@@ -293,7 +293,7 @@ int loopspec_op_linear_static(const void* W, int32_t weight_dtype, const float* 
  * as they share neither outputs nor scratch.  All pointers are device memory of the current device unless said otherwise; types: 0 = fp32, 1 = bf16,
  * 2 = fp16.  Shapes outside what is stated return LOOPSPEC_EINVAL, scratch that is missing, too small or not 256-byte aligned LOOPSPEC_ECAPACITY; neither
  * launches anything.  What only the device can see is bounds-checked there: nothing outside the cache and the tables is read or written, and
- * a flag is left - bit 0 a table entry that is no page of the cache, or a position beyond the table; bit 1 row counts that do not ascend in
+ * a flag is left (by calls that have rows and sequences) - bit 0 a table entry that is no page of the cache, or a position beyond the table; bit 1 row counts that do not ascend in
  * [0, T], or a length beyond the table; bit 2 a bounded wait that ran out. */
 
 /* Keys and values of one layer behind one set of strides: element (page, head, slot, i) of either lies at
@@ -314,7 +314,8 @@ typedef struct {
  * rotated: pairs (i, i + rot_dim / 2) of the first rot_dim elements turn by index * inv_freq[i] (fp64 [rot_dim / 2], radians per position;
  * rot_dim % 8 == 0, 0 = no rotation), index = position + pos_offset[b] (int32 [n_seqs], NULL = 0: the length of a shared prefix, say).  The angle is taken
  * in 64 bits, the rest in fp32 and rounded once to the cache's type; q_out: [T] rows of n_q_heads heads of that type, q_ld elements apart
- * (n_q_heads = 0: keys and values only).  qkv and q_out: 16-byte aligned, rows multiples of 8 elements.  Two sequences must not
+ * (n_q_heads = 0: keys and values only).  Where the row counts do not ascend (bit 1 of the flag) the rows that they give to no sequence are taken for padding,
+ * and none is written in front of cached[b].  qkv and q_out: 16-byte aligned, rows multiples of 8 elements.  Two sequences must not
  * own the same page at the positions being written.  flag: int32 that the call ors its bits into, or NULL. */
 int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv,
                           const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* cached, const int32_t* cu_rows, int32_t n_seqs,

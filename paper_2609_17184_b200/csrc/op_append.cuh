@@ -61,9 +61,11 @@ struct AppRow {
 __device__ __forceinline__ AppRow app_row(const AppendParams& p, int row, int lane, bool turns, int i0) {
   AppRow r;
   const int seq = seq_of_row(p.cu_rows, p.B, row, lane);
-  r.in = seq >= 0 && row < __ldg(p.cu_rows + max(seq, 0) + 1);
+  // (counts that do not ascend may give any answer: a row is behind the sequence's first, so nothing that is cached is written again)
+  const int at = max(seq, 0), first = __ldg(p.cu_rows + at);
+  r.in = seq >= 0 && first >= 0 && first <= row && row < __ldg(p.cu_rows + at + 1);
   if (!r.in) return r;
-  const long long pos = (long long)__ldg(p.cached + seq) + (row - __ldg(p.cu_rows + seq));
+  const long long pos = (long long)__ldg(p.cached + seq) + (row - first);
   const long long pg = pos >> p.kv.page_shift;
   int page = -1;
   if (pos >= 0 && pg < p.table_w) page = __ldg(p.page_table + seq * p.table_ld + pg);
@@ -83,6 +85,17 @@ __device__ __forceinline__ AppRow app_row(const AppendParams& p, int row, int la
     }
   }
   return r;
+}
+
+// Whether the row counts ascend within [0, T]: the first CTA asks, for all
+__device__ __forceinline__ void app_check_counts(const AppendParams& p) {
+  if (!p.err || blockIdx.x || blockIdx.y) return;
+  bool bad = false;
+  for (int i = threadIdx.x; i <= p.B; i += APP_WARPS * 32) {
+    const int c = __ldg(p.cu_rows + i);
+    bad |= c < 0 || c > p.T || (i && c < __ldg(p.cu_rows + i - 1));
+  }
+  if (bad) atomicOr(p.err, OP_BAD_ROWS);
 }
 
 // Few rows: a row's heads over the warps of one CTA or several, for what counts is the way to the last store.
@@ -109,6 +122,7 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
     }
   };
   fetch(h_warp);
+  app_check_counts(p);
 
   const AppRow its = app_row(p, row, lane, live && turns, i0);
   if (!its.in) return;  // behind the last sequence: left as it was
@@ -172,6 +186,7 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_rows_kernel(const __gri
   constexpr int HPW = 32 / LH, AHEAD = 4;
   typedef unsigned long long u64;
   const int lane = threadIdx.x & 31, row = blockIdx.x * APP_WARPS + (threadIdx.x >> 5);
+  app_check_counts(p);
   if (row >= p.T) return;
   const int d = p.kv.d, c = lane & (LH - 1), h_lane = lane / LH;
   const bool live = c < d / 8, turns = 8 * c < p.rot;

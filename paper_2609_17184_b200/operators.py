@@ -18,7 +18,8 @@ def append_kv(qkv, k_cache, v_cache, page_table, cached, cu_rows, n_q_heads, inv
     qkv [T, (n_q + 2 n_kv) d] fp32 / bf16 / fp16; k_cache, v_cache [pages, n_kv, page_size, d] bf16 / fp16 (views of any strides); page_table
     [B, W], cached [B], cu_rows [B + 1] and pos_offset [B] int32; inv_freq [rot / 2] fp64 or None (no rotation); q_norm, k_norm [d] fp32 gains
     or None (no norm).  Rows behind cu_rows[B] are left as they are in `out` and not appended.  flag: int32 tensor of one element that
-    bits are or-ed into when a page lies outside the cache (such rows are not appended)."""
+    bits are or-ed into when a page lies outside the cache (1; such rows are not appended) or row counts do not ascend within [0, T] (2; rows that they give
+    to no sequence are not appended, and nothing is written in front of cached[b])."""
     return _append_kv(qkv, k_cache, v_cache, page_table, cached, cu_rows, n_q_heads, inv_freq, q_norm, k_norm, eps, pos_offset, out, flag)
 
 

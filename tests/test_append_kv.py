@@ -209,6 +209,68 @@ def test_a_prompt_with_bad_pages_one_gain_and_numbers_that_are_none(gains):
     assert dq.all() and dkv.all()
 
 
+def counted(cu_rows, T, cached, far=0):
+    """Inputs of T rows and four or so sequences under these counts, whatever they say; every sequence has pages for `cached` positions and T more."""
+    B = len(cu_rows) - 1
+    s, g = make([T] + [0] * (B - 1), [cached] * B, 2, 1, 32, 4, "bf16", "bf16", 32, True)
+    s["table"], pages = pages_for([cached + T + far] * B, 4, np.random.default_rng(1))
+    s["kv"] = torch.randn(pages, 2, 1, 4, 32).to(torch.bfloat16)
+    s["cu"] = torch.tensor(cu_rows, dtype=torch.int32)
+    for k in ("table", "kv", "cu"):
+        g[k] = s[k].cuda()
+    return s, g
+
+
+def positions_written(s, g):
+    """[(sequence, position)] of the slots that are not what they were."""
+    moved = (g["kv"].cpu() != s["kv"]).any(4).any(2).any(1)  # [page][slot]
+    where = {int(p): (b, i) for b, row in enumerate(s["table"]) for i, p in enumerate(row)}
+    return sorted((where[int(p)][0], where[int(p)][1] * 4 + int(slot)) for p, slot in moved.nonzero())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("many", [1, 100])  # (rows of either kernel)
+@pytest.mark.parametrize("cu_rows,T", [([0, 5, 3, 8], 12), ([0, 6, 10, 2, 12], 12), ([0, 5, 20], 12), ([-3, 4, 12], 12), ([12, 9, 6, 3, 0], 12), ([2, 2, 1], 12), ([0, 4, 2 ** 31 - 1], 12),
+                                       ([0, -2 ** 31, 12], 12)])
+def test_row_counts_that_do_not_ascend_leave_a_flag_and_what_is_cached(cu_rows, T, many):
+    cached = 7 * many
+    s, g = counted([min(max(c * many, -2 ** 31), 2 ** 31 - 1) for c in cu_rows], T * many, cached, far=4 * many)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    call(g, flag=flag)
+    assert flag.item() & 2
+    assert all(pos >= cached for _, pos in positions_written(s, g))
+    g["kv"].copy_(s["kv"])
+    call(g)  # (no flag asked for)
+    assert all(pos >= cached for _, pos in positions_written(s, g))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("many", [1, 100])
+def test_row_counts_beyond_the_rows_leave_a_flag_and_append_what_there_is(many):
+    s, g = counted([0, 5 * many, 20 * many], 12 * many, 3)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    call(g, flag=flag)
+    assert flag.item() == 2
+    assert positions_written(s, g) == [(0, 3 + j) for j in range(5 * many)] + [(1, 3 + j) for j in range(7 * many)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B", [1, 127, 128, 3000])
+def test_row_counts_are_looked_at_to_the_last(B):
+    """Good counts of any number leave no flag; one bad count in any place does."""
+    s, g = make([1] + [0] * (B - 1), [0] * B, 1, 1, 8, 4, "bf16", "bf16", 8, False)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    call(g, flag=flag)
+    assert flag.item() == 0
+    for at in sorted({0, 1, B // 2, B - 1, B}):
+        for bad in (-1, 2):
+            flag.zero_()
+            g["cu"].copy_(s["cu"])
+            g["cu"][at] = bad
+            call(g, flag=flag)
+            assert flag.item() & 2, (at, bad)
+
+
 @pytest.mark.gpu
 def test_not_a_number_stays_in_its_row():
     s, g = make([3, 2], [0, 6], 2, 2, 64, 16, "fp32", "bf16", 64, True, pad=2)
