@@ -315,7 +315,7 @@ typedef struct {
  * rot_dim % 8 == 0, 0 = no rotation), index = position + pos_offset[b] (int32 [n_seqs], NULL = 0: the length of a shared prefix, say).  The angle is taken
  * in 64 bits, the rest in fp32 and rounded once to the cache's type; q_out: [T] rows of n_q_heads heads of that type, q_ld elements apart
  * (n_q_heads = 0: keys and values only).  Where the row counts do not ascend (bit 1 of the flag) the rows that they give to no sequence are taken for padding,
- * and none is written in front of cached[b].  qkv and q_out: 16-byte aligned, rows multiples of 8 elements.  Two sequences must not
+ * and none is written in front of cached[b].  What a token's row gives does not depend on the other rows of the call nor on how many there are.  qkv and q_out: 16-byte aligned, rows multiples of 8 elements.  Two sequences must not
  * own the same page at the positions being written.  flag: int32 that the call ors its bits into, or NULL. */
 int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv,
                           const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* cached, const int32_t* cu_rows, int32_t n_seqs,

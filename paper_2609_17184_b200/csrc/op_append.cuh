@@ -98,6 +98,10 @@ __device__ __forceinline__ void app_check_counts(const AppendParams& p) {
   if (bad) atomicOr(p.err, OP_BAD_ROWS);
 }
 
+// Both kernels below do a head's arithmetic in the same order, so a token's query and key are the same bits in calls of any number of rows.  A lane's
+// squares are two chains, of its even and of its odd elements:
+__device__ __forceinline__ float app_squares(float a, float b, float c, float d) { return fmaf(d, d, fmaf(c, c, fmaf(b, b, __fmul_rn(a, a)))); }
+
 // Few rows: a row's heads over the warps of one CTA or several, for what counts is the way to the last store.
 // LH: lanes per head (a power of two >= d / 8)
 template <typename TI, typename TO, int LH>
@@ -147,13 +151,11 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = b[i] = 0.f;
       if (p.q_norm || p.k_norm) {
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ss += a[i] * a[i] + b[i] * b[i];
+        float ss = app_squares(a[0], a[2], b[0], b[2]) + app_squares(a[1], a[3], b[1], b[3]);
 #pragma unroll
         for (int o = LH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         if (gain) {
-          const float r = rsqrtf(ss * inv_d + p.eps);  // (2 ulp)
+          const float r = rsqrtf(fmaf(ss, inv_d, p.eps));  // (2 ulp)
           const float4 g0 = *reinterpret_cast<const float4*>(gain + i0), g1 = *reinterpret_cast<const float4*>(gain + i1);
           a[0] *= r * g0.x, a[1] *= r * g0.y, a[2] *= r * g0.z, a[3] *= r * g0.w;
           b[0] *= r * g1.x, b[1] *= r * g1.y, b[2] *= r * g1.z, b[3] *= r * g1.w;
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float u = a[i], w = b[i];
-          a[i] = u * cs[i] - w * sn[i], b[i] = w * cs[i] + u * sn[i];
+          a[i] = fmaf(w, -sn[i], __fmul_rn(u, cs[i])), b[i] = fmaf(u, sn[i], __fmul_rn(w, cs[i]));
         }
       }
       TO* dst = nullptr;
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_rows_kernel(const __gri
               float ss = here ? s0 + s1 : 0.f;
 #pragma unroll
               for (int o = LH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-              const float r = rsqrtf(ss * inv_d + p.eps);  // (2 ulp)
+              const float r = rsqrtf(fmaf(ss, inv_d, p.eps));  // (2 ulp)
               const u64 r2 = two(r, r);
 #pragma unroll
               for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], mul2(r2, g[i]));

@@ -272,6 +272,22 @@ def test_row_counts_are_looked_at_to_the_last(B):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("tin,tc", [("fp32", "bf16"), ("bf16", "bf16"), ("fp16", "fp16")])
+@pytest.mark.parametrize("nq,nkv,d,rot", [(6, 2, 128, 128), (4, 4, 64, 32), (3, 1, 96, 96), (2, 1, 8, 8)])
+def test_a_row_is_the_same_in_calls_of_any_number_of_rows(nq, nkv, d, rot, tin, tc, norm):
+    """The same tokens among 1300 rows and among 900: queries, keys and values to the bit."""
+    s, g = make([1300], [3], nq, nkv, d, 16, tin, tc, rot, norm)
+    many = call(g).clone(), g["kv"].clone()
+    g["kv"].copy_(s["kv"])
+    g["x"], g["q"], g["cu"] = g["x"][:900], g["q"][:900], torch.tensor([0, 900], dtype=torch.int32, device="cuda")
+    q = call(g)
+    assert torch.equal(q, many[0][:900])
+    pages = s["table"][0, :903 // 16].long()
+    assert torch.equal(g["kv"][pages], many[1][pages])
+
+
+@pytest.mark.gpu
 def test_not_a_number_stays_in_its_row():
     s, g = make([3, 2], [0, 6], 2, 2, 64, 16, "fp32", "bf16", 64, True, pad=2)
     g["x"][1] = float("nan")
