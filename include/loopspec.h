@@ -332,12 +332,20 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
  * on are left as they are.  head_dim 64 or 128; n_seqs <= 2048; prefix_len >= 0.  Scores, sums and weighted values are fp32; the
  * softmax weights are rounded to the cache's type before they multiply the values.  scratch: loopspec_prefix_attention_scratch_bytes bytes (0 = not a shape it
  * takes), contents irrelevant; calls in flight at the same time need scratch of their own.  Deterministic; how the sums are cut depends on the batch.  flag:
- * int32 that the call ors its bits into, or NULL; outputs of a call that left a bit there are void where the fault lay. */
+ * int32 that the call ors its bits into, or NULL; outputs of a call that left a bit there are void where the fault lay, and NaN (lse too) where a bounded
+ * wait ran out, with a flag or without. */
 size_t loopspec_prefix_attention_scratch_bytes(int32_t T, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t prefix_len);
 int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv, const int32_t* prefix_pages,
                                  int32_t prefix_len, const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* lens,
                                  const int32_t* cu_rows, int32_t n_seqs, float scale, void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch,
                                  size_t scratch_bytes, void* cuda_stream);
+
+/* The same with a test hook: stop_tile >= 0 = the CTAs that multiply the prefix on the tensor cores (batches of more than 32 rows of a key head) request none of
+ * their 128-key tiles from this one on, and their waits give up after wait_us microseconds (<= 0: as always, some 0.2 s). */
+int loopspec_debug_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv, const int32_t* prefix_pages,
+                                    int32_t prefix_len, const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* lens,
+                                    const int32_t* cu_rows, int32_t n_seqs, float scale, void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch,
+                                    size_t scratch_bytes, void* cuda_stream, int32_t stop_tile, int32_t wait_us);
 
 /* One token for each of `rows` rows of logits (dtype 0, 1 or 2; ld elements apart), 1 <= vocab <= 262144, from one given uniform number a row (fp32 in [0, 1)).
  * A token's weight is exp((z - max z) / temperature); tokens are ranked by logit, ties by lower index first.  top_k > 0 keeps the first top_k; 0 < top_p < 1 then the

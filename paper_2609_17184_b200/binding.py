@@ -14,7 +14,7 @@ EXPORTS = ["loopspec_workspace_bytes", "loopspec_init", "loopspec_prefill", "loo
            "loopspec_get_stats", "loopspec_get_commits", "loopspec_get_row_trace", "loopspec_debug_logits",
            "loopspec_launches_per_step", "loopspec_decode_paths", "loopspec_debug_drop_tile", "loopspec_time_kernel", "loopspec_linear_scratch_bytes", "loopspec_op_linear",
            "loopspec_op_linear_static", "loopspec_linear_tc_scratch_bytes", "loopspec_op_linear_tc", "loopspec_time_linear_tc",
-           "loopspec_op_append_kv", "loopspec_prefix_attention_scratch_bytes", "loopspec_op_prefix_attention",
+           "loopspec_op_append_kv", "loopspec_prefix_attention_scratch_bytes", "loopspec_op_prefix_attention", "loopspec_debug_prefix_attention",
            "loopspec_op_sample", "loopspec_last_error", "loopspec_destroy"]
 
 STATUS = {0: "OK", -1: "EINVAL", -2: "ESTATE", -3: "ECAPACITY", -4: "ECUDA", -5: "ETIMEOUT", -6: "EUNSUPPORTED"}
@@ -103,6 +103,7 @@ def _load():
     lib.loopspec_prefix_attention_scratch_bytes.restype = C.c_size_t
     lib.loopspec_prefix_attention_scratch_bytes.argtypes = [I, I, I, I, I, I]
     lib.loopspec_op_prefix_attention.argtypes = [V, L, I, I, P(PagedKv), V, I, V, L, I, V, V, I, C.c_float, V, L, V, V, V, C.c_size_t, V]
+    lib.loopspec_debug_prefix_attention.argtypes = lib.loopspec_op_prefix_attention.argtypes + [I, I]
     lib.loopspec_op_sample.argtypes = [V, I, L, I, I, V, V, V, V, V, V, V, V]
     lib.loopspec_last_error.restype = C.c_char_p
     lib.loopspec_last_error.argtypes = [V]

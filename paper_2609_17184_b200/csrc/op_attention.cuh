@@ -30,7 +30,7 @@ constexpr int PXR_KEYS = 16;         // keys of a tile
 constexpr int PXT_ROWS = 128, PXT_KEYS = 128;
 constexpr int PXT_K_STAGES = 3, PXT_V_STAGES = 2;  // tiles of keys and of values in flight
 constexpr float PX_SLACK = 8.f;  // (log2) how far a row's maximum may run ahead of its reference
-constexpr long long PX_WAIT_CYCLES = 400000000LL;  // ~0.2 s: a wait that runs this long gives up and leaves its flag
+constexpr long long PX_WAIT_CYCLES = 400000000LL;  // ~0.2 s: a wait that runs this long gives up: its rows become NaN, and it leaves its flag
 
 template <int D>
 struct PxCfg {
@@ -67,6 +67,8 @@ struct PrefixParams {
   long long out_ld;
   float* lse;              // [T][nq] or null
   int* flag;
+  long long wait_cycles;   // how long a wait may take (PX_WAIT_CYCLES)
+  int stop_tile;           // test hook: no CTA requests its tiles of keys and values from this one on (INT_MAX: all are), so that the waits for them run out
 };
 
 // a problem: rows row0 .. row0 + n - 1 of the batch against len keys; a row that lies j-th sees the first len - (n - 1 - j) of them (all of them
@@ -149,14 +151,20 @@ __device__ __forceinline__ void px_tma_4d(unsigned dst, const CUtensorMap* map, 
                "l"(reinterpret_cast<unsigned long long>(map)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
                : "memory");
 }
-// Bounded wait; after the first failure every later one gives up at once.  Most find their phase complete: they do not read the clock.
-__device__ __forceinline__ void px_wait(unsigned long long* bar, unsigned parity, bool& ok) {
+// Bounded wait: false when it gave up.  `failed` says so to the whole CTA (before whatever this warp hands on next), whose later waits give up at once.
+// Most find their phase complete: they read neither that nor the clock.
+__device__ __forceinline__ bool px_wait(const PrefixParams& p, unsigned long long* bar, unsigned parity, int& failed) {
   unsigned done;
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                : "=r"(done)
                : "r"(tc_smem_u32(bar)), "r"(parity)
                : "memory");
-  if (!done && !tc_mbar_wait(tc_smem_u32(bar), parity, ok ? PX_WAIT_CYCLES : 2000LL)) ok = false;
+  if (!done && !tc_mbar_wait(tc_smem_u32(bar), parity, *const_cast<volatile int*>(&failed) ? 2000LL : p.wait_cycles)) {
+    *const_cast<volatile int*>(&failed) = 1;
+    __threadfence_block();
+    return false;
+  }
+  return true;
 }
 // Work is dealt as a line of U units, of which worker w of W has [w U / W, (w + 1) U / W); no worker goes empty (the slot of one without units would be
 // read, but never written), so there are at most as many as units.

@@ -47,19 +47,18 @@ __global__ void __launch_bounds__(PX_THREADS, 1)
     pxt_begin(s_tiles, tid, warp);
     tmem = s_tiles.tmem;
   }
-  bool ok = true;
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (tiles && warp == 8) pxt_produce<D, PXT_K_STAGES>(map_k, p, s_tiles.kfull, s_tiles.kempty, w.k_ring, w, lane, ok);
-    if (tiles && warp == 9) pxt_scores<T, D>(p, s_tiles, w, tmem, ok);
-    if (tiles && warp == 10) pxt_values<T, D>(p, s_tiles, w, tmem, lane, ok);
-    if (tiles && warp == 11) pxt_produce<D, PXT_V_STAGES>(map_v, p, s_tiles.vfull, s_tiles.vempty, w.v_ring, w, lane, ok);
+    if (tiles && warp == 8) pxt_produce<D, PXT_K_STAGES>(map_k, p, s_tiles.kfull, s_tiles.kempty, w.k_ring, w, lane, s_tiles.failed);
+    if (tiles && warp == 9) pxt_scores<T, D>(p, s_tiles, w, tmem);
+    if (tiles && warp == 10) pxt_values<T, D>(p, s_tiles, w, tmem, lane);
+    if (tiles && warp == 11) pxt_produce<D, PXT_V_STAGES>(map_v, p, s_tiles.vfull, s_tiles.vempty, w.v_ring, w, lane, s_tiles.failed);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    if (tiles) pxt_softmax<T, D>(p, s_tiles, w, tmem, tid, warp, lane, ok);
+    if (tiles) pxt_softmax<T, D>(p, s_tiles, w, tmem, tid, warp, lane);
     else if (base_u > 0) px_rows_role<T, D>(p, px_smem, s_unit, base_u, blockIdx.x - roles.tiles, PX_SMS - roles.tiles);
   }
-  if (tiles) pxt_end(p, tmem, warp, ok);
+  if (tiles) pxt_end(p, s_tiles, tmem, tid, warp);
 }
 
 // WPR warps per sequence and query head: a row's partials - of the prefix and of the sequence's own keys - in a fixed order, a lane looking one up each.  A

@@ -65,6 +65,7 @@ struct PxtShared {
   unsigned long long rf[2][4];         // ... references of its tile known, to a warp's rows
   unsigned long long pw[2][2], pv[2];  // ... weights there (of either half of the keys), multiplied
   unsigned tmem;
+  int failed;  // a wait has run out
   float m[2][PXT_ROWS], l[2][PXT_ROWS];
 };
 
@@ -109,14 +110,16 @@ __device__ __forceinline__ void pxt_segment_sync() {
 // Producer of the keys or of the values: a lane per box (a tile is D / 64 pieces of [128 keys][64 elements])
 template <int D, int STAGES>
 __device__ __forceinline__ void pxt_produce(const CUtensorMap& map, const PrefixParams& p, unsigned long long* full, unsigned long long* empty, unsigned ring, const PxtWork& w,
-                                            int lane, bool& ok) {
+                                            int lane, int& failed) {
   constexpr int TILE = PxCfg<D>::TC_TILE, HALF = PXT_KEYS * 128, NH = D / 64;
   const int slots = min(PXT_KEYS, 1 << p.kv.page_shift), boxes = PXT_KEYS / slots;
   const int box = lane % boxes, half = lane / boxes;
   int s = 0, units = 0;
   unsigned par = 1;
+  bool ok = true;
   w.each(p, [&](int, int h, int k_lo, int n) {
-    for (int i = 0; i < n; ++i) {
+    // (after a wait that gave up nothing more is requested: a stage may still be read, or be on its way.  Who waits for it gives up, too)
+    for (int i = 0; i < n && ok && units < p.stop_tile; ++i) {
       const int live = (w.keys(k_lo + i) + slots - 1) / slots;  // boxes with keys in them
       const int pos = (k_lo + i) * PXT_KEYS + box * slots;
       const bool mine = half < NH && box < live;
@@ -128,7 +131,10 @@ __device__ __forceinline__ void pxt_produce(const CUtensorMap& map, const Prefix
           if (p.flag) atomicOr(p.flag, OP_BAD_PAGE);
         }
       }
-      if (units >= STAGES) px_wait(empty + s, par, ok);
+      if (units >= STAGES) {
+        ok = __all_sync(0xffffffffu, px_wait(p, empty + s, par, failed));
+        if (!ok) break;
+      }
       const unsigned bar = tc_smem_u32(full + s);
       if (lane == 0) tc_mbar_expect_tx(bar, (unsigned)(live * NH * slots * 128));
       __syncwarp();
@@ -147,16 +153,17 @@ __host__ __device__ constexpr unsigned pxt_idesc(int n, bool b_mn_major) {
 // Issuers of the two products, a warp each (one for both, with five waits a tile, took 2500 cycles of it): a warp walks the tiles together, one elected
 // lane issues.  S = Q K^T of a tile into its stream's scores, as soon as the last ones there have been read:
 template <typename T, int D>
-__device__ __forceinline__ void pxt_scores(const PrefixParams& p, PxtShared& sh, const PxtWork& w, unsigned tmem, bool& ok) {
+__device__ __forceinline__ void pxt_scores(const PrefixParams& p, PxtShared& sh, const PxtWork& w, unsigned tmem) {
   constexpr int TILE = PxCfg<D>::TC_TILE, HALF = PXT_KEYS * 128;
+  bool ok = true;
   const unsigned long long desc = tc_smem_desc(0), q = desc | ((w.base >> 4) & 0x3FFF);  // 8-row groups 1024 bytes apart
   int s = 0, read[2] = {0, 0};  // ring stage; scores of a stream that have been waited for
   unsigned par = 0;
   w.each(p, [&](int, int, int, int n) {
     pxt_segment_sync();
     for (int i = 0; i < n; ++i) {
-      if (i >= 2) px_wait(&sh.sr[i & 1], read[i & 1]++ & 1, ok);
-      px_wait(&sh.kfull[s], par, ok);
+      if (i >= 2) ok &= px_wait(p, &sh.sr[i & 1], read[i & 1]++ & 1, sh.failed);
+      ok &= px_wait(p, &sh.kfull[s], par, sh.failed);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (tc_elect_one()) {
         const unsigned long long k = desc | (((w.k_ring + s * TILE) >> 4) & 0x3FFF);
@@ -170,13 +177,14 @@ __device__ __forceinline__ void pxt_scores(const PrefixParams& p, PxtShared& sh,
       __syncwarp();
       if (++s == PXT_K_STAGES) s = 0, par ^= 1u;
     }
-    for (int i = max(0, n - 2); i < n; ++i) px_wait(&sh.sr[i & 1], read[i & 1]++ & 1, ok);  // (no phase is missed)
+    for (int i = max(0, n - 2); i < n; ++i) ok &= px_wait(p, &sh.sr[i & 1], read[i & 1]++ & 1, sh.failed);  // (no phase is missed)
   });
 }
 // O += P V of a tile as its weights come, the first half of its keys while the second half's exponentials are taken:
 template <typename T, int D>
-__device__ __forceinline__ void pxt_values(const PrefixParams& p, PxtShared& sh, const PxtWork& w, unsigned tmem, int lane, bool& ok) {
+__device__ __forceinline__ void pxt_values(const PrefixParams& p, PxtShared& sh, const PxtWork& w, unsigned tmem, int lane) {
   constexpr int TILE = PxCfg<D>::TC_TILE, HALF = PXT_KEYS * 128, NH = D / 64;
+  bool ok = true;
   const unsigned long long desc = tc_smem_desc(0) | (unsigned long long)(HALF >> 4) << 16;  // 8-key groups 1024 bytes apart, the pieces of 64 elements HALF
   int s = 0, done[2] = {0, 0};  // ring stage, tiles of a stream
   unsigned par = 0;
@@ -185,7 +193,7 @@ __device__ __forceinline__ void pxt_values(const PrefixParams& p, PxtShared& sh,
     for (int i = 0; i < n; ++i) {
       const int keys = w.keys(k_lo + i), steps = (keys + 15) / 16, st = i & 1;
       const unsigned v = w.v_ring + s * TILE;
-      px_wait(&sh.vfull[s], par, ok);
+      ok &= px_wait(p, &sh.vfull[s], par, sh.failed);
       if (keys & 15) {  // values behind the last key, up to a whole step: whatever they are, 0 times them must be 0
         for (int e = lane; e < (steps * 16 - keys) * NH * 8; e += 32) {
           const int c = e & 7, x = (e >> 3) % NH, r = keys + (e >> 3) / NH;
@@ -196,7 +204,7 @@ __device__ __forceinline__ void pxt_values(const PrefixParams& p, PxtShared& sh,
       }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        px_wait(&sh.pw[st][half], done[st] & 1, ok);
+        ok &= px_wait(p, &sh.pw[st][half], done[st] & 1, sh.failed);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (tc_elect_one()) {
           const unsigned long long b = desc | ((v >> 4) & 0x3FFF);
@@ -219,7 +227,7 @@ __device__ __forceinline__ void pxt_values(const PrefixParams& p, PxtShared& sh,
 }
 
 template <typename T, int D>
-__device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh, const PxtWork& w, unsigned tmem, int tid, int warp, int lane, bool& ok) {
+__device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh, const PxtWork& w, unsigned tmem, int tid, int warp, int lane) {
   constexpr int HALF = PXT_KEYS * 128;
   int done = 0, done_other = 0;  // tiles this warp's stream has had, and the other
   w.each(p, [&](int rt, int h, int k_lo, int n) {
@@ -243,7 +251,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
     float ref = -INFINITY, l = 0.f;
     for (int j = 0; j < mine; ++j) {
       const int i = 2 * j + st;
-      px_wait(&sh.sc[st], (done + j) & 1, ok);
+      px_wait(p, &sh.sc[st], (done + j) & 1, sh.failed);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       unsigned v[4][32];
 #pragma unroll
@@ -271,13 +279,13 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
       float to = m;
       bool moves = false;
       if (i > 0) {
-        px_wait(&sh.rf[st ^ 1][warp & 3], (done_other + (st ? j : j - 1)) & 1, ok);
+        px_wait(p, &sh.rf[st ^ 1][warp & 3], (done_other + (st ? j : j - 1)) & 1, sh.failed);
         const float prev = sh.m[st ^ 1][row];
         moves = m > prev + PX_SLACK;
         to = moves ? m : prev;
         if (__any_sync(0xffffffffu, moves)) {  // the accumulator is at rest when the tile before is multiplied: this one's weights are not there yet
-          if (j > 0) px_wait(&sh.pv[st], (done + j - 1) & 1, ok);  // (tiles are multiplied in order: then the other stream's last phase but one is over)
-          px_wait(&sh.pv[st ^ 1], (done_other + (st ? j : j - 1)) & 1, ok);
+          if (j > 0) px_wait(p, &sh.pv[st], (done + j - 1) & 1, sh.failed);  // (tiles are multiplied in order: then the other stream's last phase but one is over)
+          px_wait(p, &sh.pv[st ^ 1], (done_other + (st ? j : j - 1)) & 1, sh.failed);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const float f = to == -INFINITY ? 1.f : px_exp2(prev - to);
 #pragma unroll
@@ -298,7 +306,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
       ref = to;
       const float sub = ref == -INFINITY ? 0.f : ref;
       const unsigned long long sc2 = two(p.scale_log2, p.scale_log2), sub2 = two(-sub, -sub);
-      if (j > 0) px_wait(&sh.pv[st], (done + j - 1) & 1, ok);  // this stream's last weights are used up
+      if (j > 0) px_wait(p, &sh.pv[st], (done + j - 1) & 1, sh.failed);  // this stream's last weights are used up
       unsigned long long sum[2] = {0, 0};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -324,7 +332,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
     }
     // ---- the row's partial: warps 0 .. 3 the first half of its elements, 4 .. 7 the second ----
     sh.l[st][row] = l;
-    if (mine > 0) px_wait(&sh.pv[st], (done + mine - 1) & 1, ok);
+    if (mine > 0) px_wait(p, &sh.pv[st], (done + mine - 1) & 1, sh.failed);
     done += mine, done_other += n - mine;
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -341,6 +349,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
     float* po = (k_lo == 0 ? p.tc_item_o : p.tc_work_o) + (tile * PXT_ROWS + row) * D;
     float* pm = (k_lo == 0 ? p.tc_item_ml : p.tc_work_ml) + (tile * PXT_ROWS + row) * 2;
     const bool live = r0 + row < w.R;
+    if (*const_cast<volatile int*>(&sh.failed)) mass = CUDART_NAN_F;  // whatever was multiplied: no number for a caller without a flag
     if (live && st == 0) __stcg(reinterpret_cast<float2*>(pm), make_float2(top, mass));
     if (k_lo == 0 && tid == 0) p.tc_seg[tile] = make_int2(w.worker, n == w.all ? 1 : 1 + px_worker_of((long long)(h + 1) * w.all - 1, (long long)p.kv.n_kv * w.all, w.workers) - w.worker);
 #pragma unroll
@@ -360,6 +369,7 @@ __device__ __forceinline__ void pxt_softmax(const PrefixParams& p, PxtShared& sh
 // Before the warps part: barriers, tensor memory
 __device__ __forceinline__ void pxt_begin(PxtShared& sh, int tid, int warp) {
   if (tid == 0) {
+    sh.failed = 0;
     for (int s = 0; s < PXT_K_STAGES; ++s) tc_mbar_init(tc_smem_u32(&sh.kfull[s]), 1), tc_mbar_init(tc_smem_u32(&sh.kempty[s]), 1);
     for (int s = 0; s < PXT_V_STAGES; ++s) tc_mbar_init(tc_smem_u32(&sh.vfull[s]), 1), tc_mbar_init(tc_smem_u32(&sh.vempty[s]), 1);
     for (int s = 0; s < 2; ++s) {
@@ -380,10 +390,11 @@ __device__ __forceinline__ void pxt_begin(PxtShared& sh, int tid, int warp) {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 }
 // ... and after they have met again
-__device__ __forceinline__ void pxt_end(const PrefixParams& p, unsigned tmem, int warp, bool ok) {
-  if (!ok && p.flag) atomicOr(p.flag, OP_TIMEOUT);
+__device__ __forceinline__ void pxt_end(const PrefixParams& p, PxtShared& sh, unsigned tmem, int tid, int warp) {
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  const int failed = __syncthreads_or(!ok);
+  __syncthreads();
+  const bool failed = *const_cast<volatile int*>(&sh.failed) != 0;
+  if (failed && p.flag && tid == 0) atomicOr(p.flag, OP_TIMEOUT);
   if (warp == 9) {
     // a wait that gave up may have left copies in flight: give them a bounded time to land before the memory is freed
     if (failed) {

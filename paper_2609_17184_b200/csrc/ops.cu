@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <climits>
 #include <cmath>
 #include <cstring>
 
@@ -179,6 +180,42 @@ int px_launch(PrefixParams& p, const PxPlan& t, int dtype, void* stream) {
   return launch(prefix_merge_kernel<T, D, 1>, dim3((unsigned)((heads + 3) / 4), y), 128, 0, stream, p, true);
 }
 
+// stop_tile, wait_us: see loopspec_debug_prefix_attention
+int prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv, const int32_t* prefix_pages, int32_t prefix_len,
+                     const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* lens, const int32_t* cu_rows, int32_t n_seqs, float scale,
+                     void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch, size_t scratch_bytes, void* cuda_stream, int32_t stop_tile,
+                     int32_t wait_us) {
+  PrefixParams p;
+  memset(&p, 0, sizeof p);
+  PxPlan t;
+  if (!paged_kv(kv, &p.kv) || !px_plan(T, n_seqs, n_q_heads, p.kv.n_kv, p.kv.d, prefix_len, &t) || !(scale >= 0.f) || std::isinf(scale)) return LOOPSPEC_EINVAL;
+  if (table_width < 0 || table_ld < table_width || (int64_t)table_width * kv->page_size > INT32_MAX) return LOOPSPEC_EINVAL;
+  if (T == 0 || n_seqs == 0) return LOOPSPEC_OK;  // (every row is padding)
+  const int64_t width = (int64_t)n_q_heads * p.kv.d;
+  if (!q || !aligned16(q) || q_ld % 8 || (T > 1 && q_ld < width) || !out || !aligned16(out) || out_ld % 8 || (T > 1 && out_ld < width)) return LOOPSPEC_EINVAL;
+  if (!lens || !cu_rows || (table_width && !page_table) || (prefix_len && !prefix_pages)) return LOOPSPEC_EINVAL;
+  p.G = n_q_heads / p.kv.n_kv;
+  // units of 16 keys x 16 rows of a kv head, counted in 32 bits
+  const double units = ((double)T * p.G / 16 + n_seqs) * ((double)table_width * kv->page_size / 16 + 1) + ((double)T * p.G / 16 + 1) * ((double)prefix_len / 16 + 1);
+  if (units >= 2147483648.0) return LOOPSPEC_EINVAL;
+  if (!scratch || scratch_bytes < t.total || (reinterpret_cast<uintptr_t>(scratch) & 255)) return LOOPSPEC_ECAPACITY;
+  p.q = q, p.q_ld = q_ld, p.prefix_pages = prefix_pages, p.prefix_len = prefix_len;
+  p.page_table = page_table, p.table_ld = table_ld, p.table_w = table_width, p.lens = lens, p.cu_rows = cu_rows;
+  p.B = n_seqs, p.T = T, p.nq = n_q_heads;
+  p.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)p.kv.d) : scale) * 1.4426950408889634f;
+  p.max_tiles = t.max_tiles;
+  unsigned char* sc = static_cast<unsigned char*>(scratch);
+  p.state = reinterpret_cast<int*>(sc + t.state), p.item_seg = reinterpret_cast<int2*>(sc + t.item_seg), p.tc_seg = reinterpret_cast<int2*>(sc + t.tc_seg);
+  p.item_ml = reinterpret_cast<float*>(sc + t.item_ml), p.item_o = reinterpret_cast<float*>(sc + t.item_o);
+  p.warp_ml = reinterpret_cast<float*>(sc + t.warp_ml), p.warp_o = reinterpret_cast<float*>(sc + t.warp_o);
+  p.tc_item_ml = reinterpret_cast<float*>(sc + t.tc_item_ml), p.tc_item_o = reinterpret_cast<float*>(sc + t.tc_item_o);
+  p.tc_work_ml = reinterpret_cast<float*>(sc + t.tc_work_ml), p.tc_work_o = reinterpret_cast<float*>(sc + t.tc_work_o);
+  p.out = out, p.out_ld = out_ld, p.lse = lse, p.flag = flag;
+  p.stop_tile = stop_tile >= 0 ? stop_tile : INT_MAX, p.wait_cycles = stop_tile >= 0 && wait_us > 0 ? (long long)wait_us * 2000 : PX_WAIT_CYCLES;
+  if (p.kv.d == 128) return kv->dtype == 1 ? px_launch<__nv_bfloat16, 128>(p, t, 1, cuda_stream) : px_launch<__half, 128>(p, t, 2, cuda_stream);
+  return kv->dtype == 1 ? px_launch<__nv_bfloat16, 64>(p, t, 1, cuda_stream) : px_launch<__half, 64>(p, t, 2, cuda_stream);
+}
+
 // ---- sampling ----
 constexpr int SMP_MAX_VOCAB = 1 << 18, SMP_SMEM = 200 * 1024;
 template <typename T>
@@ -236,34 +273,16 @@ int loopspec_op_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t
                                  int32_t prefix_len, const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* lens,
                                  const int32_t* cu_rows, int32_t n_seqs, float scale, void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch,
                                  size_t scratch_bytes, void* cuda_stream) {
-  PrefixParams p;
-  memset(&p, 0, sizeof p);
-  PxPlan t;
-  if (!paged_kv(kv, &p.kv) || !px_plan(T, n_seqs, n_q_heads, p.kv.n_kv, p.kv.d, prefix_len, &t) || !(scale >= 0.f) || std::isinf(scale)) return LOOPSPEC_EINVAL;
-  if (table_width < 0 || table_ld < table_width || (int64_t)table_width * kv->page_size > INT32_MAX) return LOOPSPEC_EINVAL;
-  if (T == 0 || n_seqs == 0) return LOOPSPEC_OK;  // (every row is padding)
-  const int64_t width = (int64_t)n_q_heads * p.kv.d;
-  if (!q || !aligned16(q) || q_ld % 8 || (T > 1 && q_ld < width) || !out || !aligned16(out) || out_ld % 8 || (T > 1 && out_ld < width)) return LOOPSPEC_EINVAL;
-  if (!lens || !cu_rows || (table_width && !page_table) || (prefix_len && !prefix_pages)) return LOOPSPEC_EINVAL;
-  p.G = n_q_heads / p.kv.n_kv;
-  // units of 16 keys x 16 rows of a kv head, counted in 32 bits
-  const double units = ((double)T * p.G / 16 + n_seqs) * ((double)table_width * kv->page_size / 16 + 1) + ((double)T * p.G / 16 + 1) * ((double)prefix_len / 16 + 1);
-  if (units >= 2147483648.0) return LOOPSPEC_EINVAL;
-  if (!scratch || scratch_bytes < t.total || (reinterpret_cast<uintptr_t>(scratch) & 255)) return LOOPSPEC_ECAPACITY;
-  p.q = q, p.q_ld = q_ld, p.prefix_pages = prefix_pages, p.prefix_len = prefix_len;
-  p.page_table = page_table, p.table_ld = table_ld, p.table_w = table_width, p.lens = lens, p.cu_rows = cu_rows;
-  p.B = n_seqs, p.T = T, p.nq = n_q_heads;
-  p.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)p.kv.d) : scale) * 1.4426950408889634f;
-  p.max_tiles = t.max_tiles;
-  unsigned char* sc = static_cast<unsigned char*>(scratch);
-  p.state = reinterpret_cast<int*>(sc + t.state), p.item_seg = reinterpret_cast<int2*>(sc + t.item_seg), p.tc_seg = reinterpret_cast<int2*>(sc + t.tc_seg);
-  p.item_ml = reinterpret_cast<float*>(sc + t.item_ml), p.item_o = reinterpret_cast<float*>(sc + t.item_o);
-  p.warp_ml = reinterpret_cast<float*>(sc + t.warp_ml), p.warp_o = reinterpret_cast<float*>(sc + t.warp_o);
-  p.tc_item_ml = reinterpret_cast<float*>(sc + t.tc_item_ml), p.tc_item_o = reinterpret_cast<float*>(sc + t.tc_item_o);
-  p.tc_work_ml = reinterpret_cast<float*>(sc + t.tc_work_ml), p.tc_work_o = reinterpret_cast<float*>(sc + t.tc_work_o);
-  p.out = out, p.out_ld = out_ld, p.lse = lse, p.flag = flag;
-  if (p.kv.d == 128) return kv->dtype == 1 ? px_launch<__nv_bfloat16, 128>(p, t, 1, cuda_stream) : px_launch<__half, 128>(p, t, 2, cuda_stream);
-  return kv->dtype == 1 ? px_launch<__nv_bfloat16, 64>(p, t, 1, cuda_stream) : px_launch<__half, 64>(p, t, 2, cuda_stream);
+  return prefix_attention(q, q_ld, T, n_q_heads, kv, prefix_pages, prefix_len, page_table, table_ld, table_width, lens, cu_rows, n_seqs, scale, out, out_ld, lse, flag,
+                          scratch, scratch_bytes, cuda_stream, -1, 0);
+}
+
+int loopspec_debug_prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t n_q_heads, const loopspec_paged_kv* kv, const int32_t* prefix_pages,
+                                    int32_t prefix_len, const int32_t* page_table, int64_t table_ld, int32_t table_width, const int32_t* lens,
+                                    const int32_t* cu_rows, int32_t n_seqs, float scale, void* out, int64_t out_ld, float* lse, int32_t* flag, void* scratch,
+                                    size_t scratch_bytes, void* cuda_stream, int32_t stop_tile, int32_t wait_us) {
+  return prefix_attention(q, q_ld, T, n_q_heads, kv, prefix_pages, prefix_len, page_table, table_ld, table_width, lens, cu_rows, n_seqs, scale, out, out_ld, lse, flag,
+                          scratch, scratch_bytes, cuda_stream, stop_tile, wait_us);
 }
 
 int loopspec_op_sample(const void* logits, int32_t dtype, int64_t ld, int32_t rows, int32_t vocab, const float* uniforms, const float* temperature,

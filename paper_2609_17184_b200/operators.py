@@ -35,7 +35,7 @@ def prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, 
     many own positions they hold (the new rows included) and where their rows begin.  Row j of n sees the prefix and the own positions below lens - (n
     - 1 - j).  scale: None = 1 / sqrt(d).  Rows behind cu_rows[B] are left as they are.  scratch: uint8, 256-byte aligned,
     prefix_attention_scratch_bytes (allocated here if None).  flag: int32 tensor of one element that bits are or-ed into when a page lies outside the cache
-    (1), lengths or row counts are not what they should be (2) or a bounded wait ran out (4)."""
+    (1), lengths or row counts are not what they should be (2) or a bounded wait ran out (4: the rows that waited are NaN, with a flag or without)."""
     return _prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, lens, cu_rows, scale, out, lse, scratch, flag)
 
 

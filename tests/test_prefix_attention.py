@@ -253,6 +253,48 @@ def test_flags():
         flagged(lambda s: s["cu"].fill_(0)[1::2].fill_(6 * n), 2, ok=None)  # (rows that belong to several sequences)
 
 
+def stopped(s, stop_tile, wait_us, flag, out, lse, scratch):
+    """The call with its test hook, through the C ABI."""
+    from paper_2609_17184_b200.binding import PagedKv
+    T, nq, d = s["q"].shape
+    pages, _, nkv, page, _ = s["kv"].shape
+    kv = PagedKv(s["kv"][:, 0].data_ptr(), s["kv"][:, 1].data_ptr(), s["kv"].stride(0), s["kv"].stride(2), s["kv"].stride(3), pages, page, nkv, d,
+                 1 if s["q"].dtype == torch.bfloat16 else 2)
+    return ls.lib.loopspec_debug_prefix_attention(s["q"].data_ptr(), nq * d, T, nq, C.byref(kv), s["prefix"].data_ptr(), s["P"], s["table"].data_ptr(), s["table"].stride(0),
+                                                  s["table"].size(1), s["lens"].data_ptr(), s["cu"].data_ptr(), len(s["counts"]), 0.0, out.data_ptr(), nq * d, lse.data_ptr(),
+                                                  None if flag is None else flag.data_ptr(), scratch.data_ptr(), scratch.numel(),
+                                                  torch.cuda.current_stream().cuda_stream, stop_tile, wait_us)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dt,P", [(64, "fp16", 1200), (128, "bf16", 3100), (128, "bf16", 100)])
+def test_waits_that_run_out_leave_a_flag_and_no_numbers(d, dt, P):
+    """The tensor cores' CTAs request no tile from the given one on (none at all, none beyond what the rings hold, none of the last ones).  The call ends, every
+    row of the prefix is NaN, with a flag or without, and the next call is right."""
+    B = 80
+    s = make(P, [1] * B, [20] * B, 4, 2, d, 16, dt, seed=8)
+    want, want_lse = call(s)
+    scratch = torch.empty(ls.prefix_attention_scratch_bytes(B, B, 4, 2, d, P), dtype=torch.uint8, device="cuda")
+    out, lse, flag = torch.empty_like(want), torch.empty_like(want_lse), torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert stopped(s, 10 ** 6, 200, flag, out, lse, scratch) == 0 and flag.item() == 0  # (beyond all tiles)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    for stop in (0, 1, 2, 4):
+        for f in (flag.zero_(), None):
+            assert stopped(s, stop, 200, f, out, lse, scratch) == 0
+            torch.cuda.synchronize()
+            if f is not None:
+                dropped = f.item() == 4
+                assert dropped or (f.item() == 0 and stop > 0)  # (a CTA has as many tiles as the roles leave it)
+                assert dropped or torch.equal(out, want)
+            if dropped:
+                assert out.isnan().any(-1).any() and (out.isnan().all(-1) == lse.isnan()).all()
+                assert stop > 0 or (out.isnan().all() and lse.isnan().all())
+                fine = ~lse.isnan()
+                assert torch.equal(out[fine], want[fine]) and torch.equal(lse[fine], want_lse[fine])
+            got, l = call(s, flag=flag.zero_())
+            assert flag.item() == 0 and torch.equal(got, want) and torch.equal(l, want_lse)
+
+
 @pytest.mark.gpu
 def test_dimensions_of_one_element_have_any_stride():
     s = make(13, [1], [9], 3, 1, 64, 1, "bf16", seed=12)
