@@ -64,7 +64,7 @@ class PagedKv(C.Structure):
 def _load():
     if not os.path.exists(_LIB_PATH) or _build.needs_build():
         try:
-            _build.build()
+            _build.build_library()
         except Exception as e:  # no silent fallback: the CUDA library is the product
             if not os.path.exists(_LIB_PATH):
                 raise ImportError(f"libloopspec.so is missing and could not be built: {e}") from e

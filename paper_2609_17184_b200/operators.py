@@ -2,13 +2,32 @@
 
 Tensors of one call live on one device, which need not be the current one; work goes to that device's current stream.  Shapes, types
 and strides are checked - in csrc/marshal.cpp, which asks the tensors, and in the library - before anything is launched; what is refused raises LoopSpecError."""
-import torch  # noqa: F401  (the extension below is linked against it)
+import importlib.util
+import os
 
+from . import build as _build
 from .binding import LoopSpecError, lib
-from . import _marshal
 
-_marshal.set_error(LoopSpecError)
-_append_kv, _prefix_attention, _sample = _marshal.append_kv, _marshal.prefix_attention, _marshal.sample
+_marshal = None  # the compiled marshalling, from the first call on: what needs no tensors needs no torch
+
+
+def _load():
+    global _marshal
+    import torch
+    where = os.path.dirname(torch.__file__)
+    path = _build.marshal_path(where)
+    if _build.marshal_needs_build(where):
+        try:
+            _build.build_marshal(where)
+        except Exception as e:  # (one that was made for this torch and Python serves on)
+            if not os.path.exists(path):
+                raise ImportError(f"{os.path.basename(path)} is missing and could not be built: {e}") from e
+    spec = importlib.util.spec_from_file_location(__package__ + "._marshal", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.set_error(LoopSpecError)
+    _marshal = module
+    return module
 
 
 def append_kv(qkv, k_cache, v_cache, page_table, cached, cu_rows, n_q_heads, inv_freq=None, q_norm=None, k_norm=None, eps=1e-6, pos_offset=None,
@@ -20,7 +39,7 @@ def append_kv(qkv, k_cache, v_cache, page_table, cached, cu_rows, n_q_heads, inv
     or None (no norm).  Rows behind cu_rows[B] are left as they are in `out` and not appended.  flag: int32 tensor of one element that
     bits are or-ed into when a page lies outside the cache (1; such rows are not appended) or row counts do not ascend within [0, T] (2; rows that they give
     to no sequence are not appended, and nothing is written in front of cached[b])."""
-    return _append_kv(qkv, k_cache, v_cache, page_table, cached, cu_rows, n_q_heads, inv_freq, q_norm, k_norm, eps, pos_offset, out, flag)
+    return (_marshal or _load()).append_kv(qkv, k_cache, v_cache, page_table, cached, cu_rows, n_q_heads, inv_freq, q_norm, k_norm, eps, pos_offset, out, flag)
 
 
 def prefix_attention_scratch_bytes(T, n_seqs, n_q_heads, n_kv_heads, head_dim, prefix_len):
@@ -36,7 +55,7 @@ def prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, 
     - 1 - j).  scale: None = 1 / sqrt(d).  Rows behind cu_rows[B] are left as they are.  scratch: uint8, 256-byte aligned,
     prefix_attention_scratch_bytes (allocated here if None).  flag: int32 tensor of one element that bits are or-ed into when a page lies outside the cache
     (1), lengths or row counts are not what they should be (2) or a bounded wait ran out (4: the rows that waited are NaN, with a flag or without)."""
-    return _prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, lens, cu_rows, scale, out, lse, scratch, flag)
+    return (_marshal or _load()).prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, lens, cu_rows, scale, out, lse, scratch, flag)
 
 
 def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None):
@@ -46,4 +65,4 @@ def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=Non
     temperature, top_p, min_p fp32 [rows] and top_k int32 [rows], or None (1, off, off, off): the filters apply in the order top-k, top-p
     (of what top-k kept), min-p; a temperature of 0 is the first of the largest logits.  -inf and NaN are masked out; a row of nothing else gets
     token -1."""
-    return _sample(logits, uniforms, temperature, top_k, top_p, min_p, out, probs)
+    return (_marshal or _load()).sample(logits, uniforms, temperature, top_k, top_p, min_p, out, probs)
