@@ -329,7 +329,8 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
  * The prefix's keys and values are read and multiplied once for all sequences.  A row that sees no key gets zeros (lse -inf).  Keys and values behind
  * what a row sees do not enter it, whatever they hold.  q, out: [T] rows of n_q_heads heads of the cache's type, q_ld / out_ld
  * elements apart, 16-byte aligned, multiples of 8 elements; lse: fp32 [T][n_q_heads], the natural logarithm of the sum of the exponentials, or NULL.  Rows from cu_rows[n_seqs]
- * on are left as they are.  head_dim 64 or 128; n_seqs <= 2048; prefix_len >= 0.  Scores, sums and weighted values are fp32; the
+ * on are left as they are.  head_dim 64 or 128; n_seqs <= 2048; T * n_q_heads <= 2^27, n_seqs * n_q_heads <= 2^30, n_kv_heads <= 65535; prefix_len
+ * and table_width * page_size from 0 to 2^31 - 129 (and together not more than 2^31 pieces of 16 rows of a key head x 16 positions).  Scores, sums and weighted values are fp32; the
  * softmax weights are rounded to the cache's type before they multiply the values.  scratch: loopspec_prefix_attention_scratch_bytes bytes (0 = not a shape it
  * takes), contents irrelevant; calls in flight at the same time need scratch of their own.  Deterministic; how the sums are cut depends on the batch.  flag:
  * int32 that the call ors its bits into, or NULL; outputs of a call that left a bit there are void where the fault lay, and NaN (lse too) where a bounded

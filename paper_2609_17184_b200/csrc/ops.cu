@@ -102,10 +102,11 @@ struct PxPlan {
   int max_tiles, tc_tiles;
   size_t state, item_seg, tc_seg, item_ml, item_o, warp_ml, warp_o, tc_item_ml, tc_item_o, tc_work_ml, tc_work_o, total;
 };
+constexpr int PX_MAX_LEN = INT32_MAX - 128;  // positions: a tile's last still has a number
 constexpr int PXT_MIN_ROWS = 33;  // rows of the batch and a kv head from which on the prefix goes to the tensor cores' tiles
 bool px_plan(int T, int B, int nq, int nkv, int d, int P, PxPlan* o) {
   if (T < 0 || B < 0 || B > PX_MAX_SEQS || nq < 1 || nkv < 1 || nq % nkv || (d != 64 && d != 128) || P < 0) return false;
-  if ((int64_t)T * nq > (1 << 27) || nkv > 65535) return false;
+  if ((int64_t)T * nq > (1 << 27) || nkv > 65535 || (int64_t)B * nq > (1 << 30) || P > PX_MAX_LEN) return false;
   const int rows = T * (nq / nkv);
   o->max_tiles = rows / 16 + B + 1 + (P > 0 ? rows / 16 + 1 : 0);
   o->tc_tiles = rows >= PXT_MIN_ROWS && P > 0 ? (rows + PXT_ROWS - 1) / PXT_ROWS : 0;
@@ -189,7 +190,7 @@ int prefix_attention(const void* q, int64_t q_ld, int32_t T, int32_t n_q_heads, 
   memset(&p, 0, sizeof p);
   PxPlan t;
   if (!paged_kv(kv, &p.kv) || !px_plan(T, n_seqs, n_q_heads, p.kv.n_kv, p.kv.d, prefix_len, &t) || !(scale >= 0.f) || std::isinf(scale)) return LOOPSPEC_EINVAL;
-  if (table_width < 0 || table_ld < table_width || (int64_t)table_width * kv->page_size > INT32_MAX) return LOOPSPEC_EINVAL;
+  if (table_width < 0 || table_ld < table_width || (int64_t)table_width * kv->page_size > PX_MAX_LEN) return LOOPSPEC_EINVAL;
   if (T == 0 || n_seqs == 0) return LOOPSPEC_OK;  // (every row is padding)
   const int64_t width = (int64_t)n_q_heads * p.kv.d;
   if (!q || !aligned16(q) || q_ld % 8 || (T > 1 && q_ld < width) || !out || !aligned16(out) || out_ld % 8 || (T > 1 && out_ld < width)) return LOOPSPEC_EINVAL;
@@ -243,7 +244,7 @@ int loopspec_op_append_kv(const void* qkv, int32_t qkv_dtype, int64_t qkv_ld, in
                           void* q_out, int64_t q_ld, int32_t* flag, void* cuda_stream) {
   AppendParams p;
   memset(&p, 0, sizeof p);
-  if (!paged_kv(kv, &p.kv) || qkv_dtype < 0 || qkv_dtype > 2 || T < 0 || n_seqs < 0 || n_q_heads < 0 || n_q_heads > 65536 || p.kv.n_kv > 65536) return LOOPSPEC_EINVAL;
+  if (!paged_kv(kv, &p.kv) || qkv_dtype < 0 || qkv_dtype > 2 || T < 0 || T > INT32_MAX - APP_WARPS || n_seqs < 0 || n_q_heads < 0 || n_q_heads > 65536 || p.kv.n_kv > 65536) return LOOPSPEC_EINVAL;
   if ((q_norm && !aligned16(q_norm)) || (k_norm && !aligned16(k_norm))) return LOOPSPEC_EINVAL;
   if (rot_dim < 0 || rot_dim > p.kv.d || rot_dim % 8 || (rot_dim && !inv_freq)) return LOOPSPEC_EINVAL;
   if (table_width < 0 || table_ld < table_width) return LOOPSPEC_EINVAL;

@@ -354,6 +354,16 @@ def test_refusals():
     assert rc(T=0) == 0 and rc(B=0) == 0  # nothing to do
 
 
+def test_more_rows_than_can_be_counted_are_refused():
+    """Rows are counted in 32 bits, four to a CTA: the last numbers would come round to negative rows."""
+    from paper_2609_17184_b200.binding import PagedKv
+    import ctypes as C
+    A = 1 << 20
+    kv = PagedKv(A, A, 2048, 1024, 64, 4, 16, 1, 64, 1)
+    for T in (2 ** 31 - 1, 2 ** 31 - 3):
+        assert ls.lib.loopspec_op_append_kv(A, 1, 256, T, 2, C.byref(kv), A, 4, 4, A, A, 1, None, A, 64, None, None, 1e-6, A, 128, None, None) == -1
+
+
 def test_wrapper_refuses_what_is_not_a_device_tensor():
     s, g = make([1], [0], 2, 1, 64, 16, "bf16", "bf16", 64, False, dev="cpu")
     with pytest.raises(ls.LoopSpecError) as e:

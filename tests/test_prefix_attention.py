@@ -341,6 +341,19 @@ def test_refusals():
         assert ls.prefix_attention_scratch_bytes(*bad) == 0
 
 
+def test_sizes_that_cannot_be_counted_are_refused():
+    """Positions and a grid's sequences x heads are counted in 32 bits, positions in tiles of up to 128."""
+    from paper_2609_17184_b200.binding import PagedKv
+    A = 1 << 20
+    assert ls.prefix_attention_scratch_bytes(1, 2048, 1 << 20, 1, 64, 0) == 0
+    for P in (2 ** 31 - 1, 2 ** 31 - 100):
+        assert ls.prefix_attention_scratch_bytes(1, 1, 1, 1, 64, P) == 0
+    for page, width in ((1, 2 ** 31 - 1), (2, 2 ** 30 - 1), (4, 2 ** 29 - 2)):
+        assert ls.lib.loopspec_op_prefix_attention(A, 64, 1, 1, C.byref(PagedKv(A, A, 2048, 1024, 64, 4, page, 1, 64, 1)), None, 0, A, width, width, A, A, 1, 0.0, A, 64, None,
+                                                   None, A, 1 << 40, None) == -1
+    assert ls.prefix_attention_scratch_bytes(1, 2048, 1 << 18, 1, 64, 0) > 0 and ls.prefix_attention_scratch_bytes(1, 1, 1, 1, 64, 2 ** 31 - 256) > 0
+
+
 @pytest.mark.gpu
 def test_wrapper_refusals():
     def fails(status="EINVAL", call_kw={}, **kw):
