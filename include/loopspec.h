@@ -354,8 +354,10 @@ int loopspec_debug_prefix_attention(const void* q, int64_t q_ld, int32_t T, int3
  * weight.  The token is the first, by index, at which the running sum of the kept weights exceeds uniform times their sum; its probability is its weight over that
  * sum.  temperature <= 0 (or no number): the first of the largest logits, probability 1.  temperature, top_k, top_p, min_p: one value a row, or NULL for
  * 1 / 0 / 1 / 0 throughout; other values than the stated switch a filter off.  A logit of -inf, or no number, is masked out; several of +inf share
- * the weight; a row with nothing left gets token -1, probability 0.  Weights are taken in 64 bits and summed exactly, in multiples of 2^-S of the largest with S = min(48, 61 -
- * ceil(log2 vocab)): the token is the one of the definition, whatever the order.  logits: any alignment of its type.  probs: NULL if not wanted. */
+ * the weight; a row with nothing left gets token -1, probability 0.  Weights are taken in 64 bits (to 1.4e-13 of each), rounded to multiples of 2^-S of the largest with S = min(48, 61 -
+ * ceil(log2 vocab)) and summed exactly, so no order of additions shows in the token.  What rounds to nothing, a weight below 2^-(S + 1) of the largest, counts as masked out
+ * (a uniform of 0 takes the first token that does not), and the sums that decide - u's, and top-p's - are off by at most vocab * 2^-(S + 1) of the largest weight (2^-36 for
+ * 8192 tokens, 2^-26 for 262144): nearer to a border than that, the token may be a neighbour of the definition's.  logits: any alignment of its type.  probs: NULL if not wanted. */
 int loopspec_op_sample(const void* logits, int32_t dtype, int64_t ld, int32_t rows, int32_t vocab, const float* uniforms, const float* temperature,
                        const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens, float* probs, void* cuda_stream);
 

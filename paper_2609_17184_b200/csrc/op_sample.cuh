@@ -1,10 +1,10 @@
 // One token per row of logits by temperature, top-k, top-p and min-p from a given uniform number: w = exp((z - max) / T), ranked by logit (ties:
 // lower index first); the token is the first, by index, at which the running sum of the kept weights exceeds u times their sum.
 //
-// Which side of a border a sum lies on decides the token, so no sum may depend on the order of its additions or lose what a 64-bit
-// evaluation keeps: a weight is evaluated in fp64 (2^y by a table of 2^(j/256) and a polynomial of degree 3: 1.4e-13) and rounded ONCE to a multiple
+// Which side of a border a sum lies on decides the token, so no sum may depend on the order of its additions: a weight is evaluated in fp64 (2^y by a table of 2^(j/256) and a polynomial of degree 3: 1.4e-13) and rounded ONCE to a multiple
 // of 2^-S, S = 61 - ceil(log2 V) (44 at 128K tokens, 48 at most); from there on everything - sums over the vocabulary, p times a sum, u times a sum -
-// is exact integer arithmetic.  Sums are the same in every order and for every number of CTAs.  A token below 2^-(S+1) of the best weighs nothing.
+// is exact integer arithmetic.  Sums are the same in every order and for every number of CTAs.  A token below 2^-(S+1) of the best weighs nothing, and a sum is off by
+// at most V 2^-(S+1) of the best (2^-26 for the largest vocabulary, 2^-36 for 8192 tokens): a uniform number in fp32 is one of 2^-24 apart at 1.
 //
 // A cluster of CTAs holds a row in shared memory, so the logits are read from HBM once; what bounds a call is then the chain of passes over
 // a CTA's slice and of hand-overs in the cluster (some 1000 cycles each):

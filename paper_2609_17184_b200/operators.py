@@ -63,6 +63,6 @@ def sample(logits, uniforms, temperature=None, top_k=None, top_p=None, min_p=Non
     their probabilities fp32 [rows]).
 
     temperature, top_p, min_p fp32 [rows] and top_k int32 [rows], or None (1, off, off, off): the filters apply in the order top-k, top-p
-    (of what top-k kept), min-p; a temperature of 0 is the first of the largest logits.  -inf and NaN are masked out; a row of nothing else gets
-    token -1."""
+    (of what top-k kept), min-p; a temperature of 0 is the first of the largest logits.  -inf and NaN are masked out, and so is a token below 2^-(S + 1) of the
+    largest weight, S = min(48, 61 - ceil(log2 V)); a row of nothing else gets token -1."""
     return (_marshal or _load()).sample(logits, uniforms, temperature, top_k, top_p, min_p, out, probs)

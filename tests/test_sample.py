@@ -265,6 +265,74 @@ def test_offsets_beyond_32_bits():
     check(z, u, call(z, u, None, None, np.float32([0.9] * 3)), None, None, np.float32([0.9] * 3))
 
 
+def resolution(V):
+    """(2^-S, V * 2^-(S + 1)): what weights are multiples of, in parts of the largest, and what a sum of V of them is off by at most."""
+    S = min(48, 61 - max(0, (V - 1).bit_length()))
+    return 2.0 ** -S, V * 2.0 ** -(S + 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [2, 5000, 8193, 50001, 262144])
+@pytest.mark.parametrize("t", [1.0, 0.3])
+def test_tokens_below_half_a_step_of_the_largest_count_as_masked_out(V, t):
+    """A uniform of 0 takes the first token that weighs anything.  Logits by 2 % of a weight to either side of half a step (a weight is off by 1.4e-13 of itself, a logit of
+    that size by 2^-19 of the weight's logarithm)."""
+    unit, _ = resolution(V)
+    border = math.log(unit / 2) * t
+    z = torch.full((4, V), -1e4, device="cuda")
+    z[:, V - 1] = 0.0
+    z[0, 0], z[1, 0] = border + 0.02 * t, border - 0.02 * t
+    z[2, 0] = z[3, 0] = border - 0.02 * t
+    if V > 2:
+        z[2, V // 2] = border + 0.02 * t
+    ts, u = np.float32([t] * 4), np.float32([0.0] * 4)
+    for k, p, m in ((None,) * 3, ([0, V, 10 ** 9, V - 1] if V > 2 else [0, 2, 2, 2], None, None), (None, None, np.float32([1e-30] * 4))):
+        tok, prob = call(z, u, ts, k, p, m)
+        if m is None:
+            assert tok.tolist() == [0, V - 1, V // 2, V - 1]
+            assert prob[1] == 1.0 and prob[3] == 1.0 and prob[0] < unit
+        else:
+            assert tok[1] == V - 1 and tok[3] == V - 1  # (nor does min-p bring it back)
+    masked = z.masked_fill(z < border, -math.inf)
+    u = np.float32([0.0, 0.25, 0.5, 0.999])
+    for a, b in zip(call(z, u, ts), call(masked, u, ts)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [5000, 50001, 131072, 262144])
+@pytest.mark.parametrize("off", [-0.6, -0.01, 0.0, 0.01, 0.4, 3.0])
+def test_how_far_a_heavy_tail_moves_a_border(V, off):
+    """Thousands of tokens about half a step of the largest weight: each rounds the same way.  The token drawn is the definition's or one whose border is
+    nearer than a sum can be off: V * 2^-(S + 1) of the largest weight, and 1.4e-13 of the sum; and so is the last token that top-p keeps."""
+    unit, bound = resolution(V)
+    rng = np.random.default_rng(V)
+    rows = 16
+    z = np.full((rows, V), math.log(unit / 2) + off, np.float32)
+    z[:, rng.integers(0, V, 40)] = rng.uniform(-12, -3, 40)
+    z[:, V // 3] = 0.0
+    w = np.exp(z[0].astype(np.float64))
+    run = np.cumsum(w)
+    bound = bound + 1.4e-13 * run[-1]
+    at = run[rng.integers(0, V, rows)] / run[-1]
+    at[:5] = run[V // 3 - 1] / run[-1] * np.array([0.3, 0.9, 1.0, 1.1, 3.0])  # (about the largest token's border)
+    u = np.float32(np.clip(at, 0, 1 - 2.0 ** -24))
+    tok = call(torch.from_numpy(z).cuda(), u)[0].cpu().numpy()
+    at = u.astype(np.float64) * run[-1]
+    want = np.minimum(np.searchsorted(run, at, side="right"), V - 1)
+    edge = np.minimum(at - (run[want] - w[want]), run[want] - at)
+    assert (tok == want)[edge > bound].all() and (edge[:5] > bound).any()
+    assert (run[tok] - w[tok] <= at + bound).all() and (run[tok] >= at - bound).all()
+    # the same weights in the order of the ranking: a uniform of 1 takes the last token kept
+    z = -np.sort(-z, axis=1)
+    w = np.exp(z[0].astype(np.float64))
+    run = np.cumsum(w)
+    p = np.float32(np.concatenate([1 - 2.0 ** -np.arange(8, 24), [0.5] * (rows - 16)]))
+    last = call(torch.from_numpy(z).cuda(), np.float32([1.0] * rows), None, None, p)[0].cpu().numpy()
+    goal = p.astype(np.float64) * run[-1]
+    assert (run[last] >= goal - bound).all() and (run[last] - w[last] < goal + bound).all()
+
+
 def test_no_cta_reaches_into_another_before_all_of_its_cluster_have_started():
     """Read off the source, for what it prevents is a fault: every CTA of a cluster arrives at its barrier, and waits there ahead of the first exchange (a
     reduction, or an address in another CTA's shared memory)."""
