@@ -33,3 +33,18 @@ def test_two_ctas_of_sample_kernel_share_an_sm(tmp_path):
     decls = [f"smp::sample_kernel<{t}>(const __grid_constant__ smp::Params)" for t in ("float", "__nv_bfloat16", "__half")]
     found = used(tmp_path, "op_sample.cuh", decls)
     assert all(regs <= 64 for _, _, regs in found), found
+
+
+@pytest.mark.skipif(not os.path.exists(NVCC), reason="no nvcc")
+def test_what_the_kernels_keep_in_local_memory_stays_small(tmp_path):
+    """Registers are bounded by the launch (168 and 64 a thread), so what a kernel needs beyond them shows in its spills: bytes stored, 96 in the sampler and 128 in
+    prefix_kernel at most, none in the others."""
+    sample = [f"smp::sample_kernel<{t}>(const __grid_constant__ smp::Params)" for t in ("float", "__nv_bfloat16", "__half")]
+    prefix = [f"prefix_kernel<{t}, {d}>(const __grid_constant__ CUtensorMap, const __grid_constant__ CUtensorMap, const __grid_constant__ PrefixParams)"
+              for t in ("__nv_bfloat16", "__half") for d in (64, 128)]
+    fold = [f"prefix_merge_kernel<__half, {d}, {w}>(const __grid_constant__ PrefixParams)" for d in (64, 128) for w in (1, 4)]
+    append = [f"{k}<{t}, __nv_bfloat16, {lh}>(const __grid_constant__ AppendParams)" for k in ("append_kernel", "append_rows_kernel") for t in ("float", "__nv_bfloat16")
+              for lh in (8, 16, 32)]
+    for header, decls, most in (("op_sample.cuh", sample, 96), ("op_prefix.cuh", prefix, 128), ("op_prefix.cuh", fold, 0), ("op_append.cuh", append, 0)):
+        found = used(tmp_path, header, decls)
+        assert all(spill <= most for _, spill, _ in found), found
