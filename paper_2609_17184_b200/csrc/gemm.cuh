@@ -472,6 +472,7 @@ __global__ void __launch_bounds__(GEMM_THREADS) __maxnreg__(NG == 1 ? LS_MAXREG 
   auto drain = [&]() { cp_async_wait<0>(); };
 #pragma unroll 1
   for (int s = 0; s < RING - 1; ++s) issue_unit();
+  if (cs > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");  // partial sums go to other CTAs only once all have started
 
   // the row table was written before this pass started, so the live row count can be read ahead of the predecessor
   const RowTable* tab = p.tab;
@@ -481,6 +482,7 @@ __global__ void __launch_bounds__(GEMM_THREADS) __maxnreg__(NG == 1 ? LS_MAXREG 
   // the weights above are constants; everything below reads what earlier kernels of the pass produced
   stamp();
   pdl_wait();
+  if (cs > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // (long past)
   stamp();
   timeline_mark(p.tl, p.tl_id + 256, false);
   if (n_cols <= 0) {  // uniform over the cluster: nobody reaches a cluster barrier

@@ -367,6 +367,7 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(const __grid_consta
     pdl_wait();
     return;
   }
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");  // values go to other CTAs only once all have started
   const int V = p.V, tid = threadIdx.x;
   const bool writer = R.rank == 0 && tid == 0;  // all CTAs of the cluster hold the same results; one thread stores them
   // this CTA's slice of the vocabulary: whole Philox blocks of 4 indices
@@ -442,6 +443,7 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(const __grid_consta
   };
 
   pdl_wait();
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");  // (long past)
   if (kind == RO_TARGET) {
     int tok;
     if (T == 0.f) {
