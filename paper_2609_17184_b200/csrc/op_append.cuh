@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(APP_WARPS * 32) append_kernel(const __grid_con
 
 // Many rows: a warp per row, so that look-ups and sines are taken once for all heads.  Bound by the instructions per head as much as by the traffic (a loop
 // over all heads alike issued 170 a turn and took 48 us for 9,200 rows of 48 heads), so queries, keys and values have a loop each: values move as they
-// are, gains and addresses stay in registers, and the arithmetic is packed in pairs: 42 us, 4.6 TB/s, with norms or without - what is left is the
+// are, gains and addresses stay in registers, and the arithmetic is packed in pairs (in the order of the kernel above): 42 us, 4.6 TB/s, with norms or without - what is left is the
 // way of a row, four dependent look-ups ahead of its first store, in less than three rows per warp place.  More warps with fewer loads in flight each: +5 to +15 %.
 template <typename TI, typename TO, int LH>
 __global__ void __launch_bounds__(APP_WARPS * 32) append_rows_kernel(const __grid_constant__ AppendParams p) {

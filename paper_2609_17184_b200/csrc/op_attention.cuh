@@ -13,7 +13,8 @@
 // where the stream alone takes 57 and the prefix alone 62; side by side they take 102.)
 //
 // Scores are bf16 / fp16 products summed in fp32; maximum, sum and weighted values are fp32.  The softmax weights are rounded to the cache's
-// type for the second contraction: an error of half a step of the output's own type per weight, averaged over the keys.
+// type for the second contraction: an error of half a step of the output's own type per weight, averaged over the keys (large batches in
+// bf16: 0.0023 from 64 bits where weights in 32 bits leave 0.0017, the rounding of the output; fp16 0.00026 and 0.00021).
 #pragma once
 #include <cuda.h>
 

@@ -16,7 +16,9 @@
 // 128 x 128 tiles saturate) and its 16,384 exponentials, at 16 a cycle, as many.  It takes 1570: a stream's tile is a chain of about 3100 (scores
 // 100, their read 250, maximum 500, reference 500, weights 1400, hand-over), and there are two streams.  384 rows of 16 heads against 16,384 keys
 // take 63 us, 0.8 PFLOP/s.  Measured and left out: a quarter of the exponentials by a polynomial on the FMA pipe (no change; half: 5 %
-// slower), two threads per row (no change).
+// slower), two threads per row (no change).  Not measured: an accumulator per stream (weights in the place of their scores, two accumulators: 512 columns as well),
+// which would take the hand-over of the reference out of the chain.  The 168 registers of the launch are not enough for it all: 68 bytes a thread are spilled at
+// head size 128, 100 at 64, all in this role's softmax.
 #pragma once
 #include "op_attention.cuh"
 

@@ -13,7 +13,7 @@
 //   3  histogram over the distance from the best: tokens and places in a bin   other rows with top-k or top-p
 //   4  exact mass, tokens of the bins where top-p may cut                      rows with top-p
 //   5  exact mass of what stays, by index                                      all rows of many kept tokens
-// 256 rows of 50,001 16-bit logits with k = 50 take 27 us (41 by way of the histogram), 64 rows of 128,256 with settings of their own 69 us, one row of
+// 256 rows of 50,001 16-bit logits with k = 50 take 28 us (41 by way of the histogram), 64 rows of 128,256 with settings of their own 70 us, one row of
 // 49,152 with top-p 22 us, 8 rows without filters 8 us.  Measured and left out: 1024 threads a CTA (+5 to +100 %), logits left in the L2 instead of shared
 // memory (+10 to +20 % a pass), sorting up to 512 candidates instead of comparing up to 256 with each other (+30 %).
 #pragma once

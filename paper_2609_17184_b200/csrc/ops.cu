@@ -1,5 +1,6 @@
 // C ABI of the operators between the linear maps (see include/loopspec.h): checks of the arguments, rules that choose a kernel's
-// variant, launches.  No call synchronises, allocates or keeps anything.
+// variant, launches.  No call synchronises, allocates or keeps anything (but which kernels may use how much shared memory, and the driver's
+// function that encodes tensor maps).
 #include "../../include/loopspec.h"
 
 #include <algorithm>
@@ -72,9 +73,10 @@ AppendFn append_fn(int dtype, int lh, bool rows) {
 }
 
 constexpr int kSms = 148;
-// Token rows from which append_kv gives each a warp of its own; below, a row's heads are spread over warps [us spread / a warp each: 48 heads of 128 with
-// norms 300 rows 5.9 / 7.9, 600 6.9 / 8.8, 1000 10.0 / 9.2, 1990 15.4 / 11.8, 8000 50 / 36; 48 heads of 64 without 300 5.0 / 4.3, 600 4.6 / 4.9, 1000
-// 6.4 / 5.1, 1990 9.0 / 6.1]
+// Token rows from which append_kv gives each a warp of its own; below, a row's heads are spread over warps [us spread / a warp each, 16 bits: 48 heads of 128 with
+// norms 100 rows 3.8 / 7.7, 300 5.6 / 7.7, 600 6.6 / 8.6, 1000 9.7 / 8.8, 1990 14.8 / 11.5, 8000 50 / 36; 48 heads of 64 with norms 300 5.1 / 5.5, 600 5.0 / 6.1, 1000
+// 6.7 / 6.0; without 300 4.8 / 4.5, 600 4.4 / 4.9, 1000 5.9 / 5.0; 6 heads of 64 100 3.0 / 3.5, 600 3.8 / 3.9, 1000 5.0 / 3.8, 8000 20 / 10: the crossing lies
+// between 600 and 1000 rows throughout, but for 300 rows of heads of 64 without norms, which the rule costs 0.3 us]
 constexpr int APP_ROWS = 1000;
 
 // Lets a kernel ask for `bytes` of dynamic shared memory; `done` remembers, a bit per device, that it may.  regs: registers a thread that it must have
@@ -223,8 +225,8 @@ template <typename T>
 int smp_launch(smp::Params& p, void* stream) {
   static std::atomic<unsigned long long> allowed;
   constexpr int extra = 32 + smp::BINS * 8 + (smp::LIST + 2 * smp::SOLO) * 8;
-  // CTAs per row: up to three for every two SMs (two share one; a cluster's hand-overs cost more than a wider one gains: 64 rows of 32,000 take 15 us
-  // with two each, 18 with four), none with less than 2048 tokens; more where a slice would not fit
+  // CTAs per row: up to three for every two SMs (two share one; a cluster's hand-overs cost more than a wider one gains: 64 rows of 32,000 take 10.2 us
+  // with two each, 11.4 with four; with top-p 0.9 32 and 38, with k = 50 13.6 and 17.4), none with less than 2048 tokens; more where a slice would not fit
   int cs = 1;
   while (cs < smp::MAX_CS && ((p.V > 2048 * cs && p.rows * cs * 2 <= kSms * 3 / 2) || (p.V / cs + 8) * (int)sizeof(T) + extra > SMP_SMEM)) cs *= 2;
   p.per = ((p.V + cs - 1) / cs + 7) / 8 * 8;
